@@ -276,6 +276,83 @@ size_t     zgr_cloud_backward_workspace(const zgr_ctx* ctx, int32_t batch, int32
 zgr_status zgr_cloud_backward(zgr_ctx* ctx, const zgr_batch* batch, float* const* grads, int32_t n_grads, double* loss_out,
                               void* workspace, size_t workspace_bytes);
 
+/* ---- the attention sublayer of present-day blocks, operator by operator (no context, no model: any shapes) ----
+ * Norms of queries and keys for each head with the position rotation; attention with a learned relative position bias; dropout with
+ * the residual sum; each with its gradient.  All tensors are DEVICE, in dtype (zgr_dtype) unless stated; every sum, softmax statistic and norm
+ * is held in fp32 and a result is rounded once.  Asynchronous on hip_stream, no allocation, no synchronisation, no state kept between
+ * calls; two runs give the same bits.  A workspace is DEVICE memory on 256 bytes that one call at a time uses.  ZGR_ERR_* as above, the message from
+ * zgr_last_error(NULL); a call that returns one has launched nothing (ZGR_ERR_DEVICE: nothing after the launch that failed).              */
+
+/* Heads of tokens: entry c of head h of token t of sequence b at data + b batch + t token + h head + c (strides in ENTRIES, any order; data on 16 bytes,
+ * strides multiples of 16 bytes).  Columns of a projection's output, a cache by tokens and one by heads are all such views.                            */
+typedef struct { void* data; int64_t batch, token, head; } zgr_heads;
+
+/* y = gain x / sqrt(mean(x^2) + eps) over the head_dim entries of each head, then the pairs (a, b) of its first rot_dim entries turned by their
+ * position's angle: (a cos - b sin, b cos + a sin).  Pairs are entries (i, i + rot_dim / 2), or (2 i, 2 i + 1) with interleaved = 1.            */
+typedef struct {
+  int32_t dtype, rows;              /* rows: tokens (zgr_heads.batch is not used)                     */
+  int32_t q_heads, k_heads;         /* either may be 0                                                */
+  int32_t head_dim;                 /* a multiple of 8 up to 256                                      */
+  int32_t rot_dim;                  /* a multiple of 8 up to head_dim; 0: no rotation                 */
+  int32_t interleaved, n_positions;
+  float   eps;
+  const void*    q_gain;            /* [head_dim]; NULL: q is not normalised                          */
+  const void*    k_gain;
+  const float*   table;             /* fp32 [n_positions][rot_dim / 2][2]: cos and sin of each pair   */
+  const int32_t* positions;         /* [rows]; one outside [0, n_positions) makes its rotated entries NaN */
+} zgr_rotation;
+
+/* Outputs may be the inputs (then the gradient's inputs are gone).                                             */
+zgr_status zgr_norm_rotate(const zgr_rotation* how, const zgr_heads* q, const zgr_heads* k, const zgr_heads* q_out, const zgr_heads* k_out, void* hip_stream);
+/* dq, dk: the gradients of q and k (which may lie where dq_out, dk_out, the gradients of the outputs, do).  dgains: fp32 [2][head_dim], the gradients of q_gain and
+ * k_gain (zeros for one that is NULL), or NULL.                                                                */
+size_t     zgr_norm_rotate_backward_workspace(const zgr_rotation* how);
+zgr_status zgr_norm_rotate_backward(const zgr_rotation* how, const zgr_heads* dq_out, const zgr_heads* dk_out, const zgr_heads* q, const zgr_heads* k, const zgr_heads* dq, const zgr_heads* dk,
+                                    float* dgains, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+#define ZGR_MAX_REACH 1024
+/* The usual map from relative positions key - query in [-reach, reach] to buckets (HOST arithmetic, map: HOST [2 reach + 1]): half of a direction's buckets hold one
+ * distance each, the rest grow with the logarithm of the distance up to reach.  causal = 1: all buckets are for keys before the query (and at it);
+ * 0: the lower half is, the upper half is for keys behind it.                                                  */
+zgr_status zgr_relative_buckets(int32_t buckets, int32_t reach, int32_t causal, int32_t* map);
+
+/* out_i = sum_j softmax_j(scale q_i . k_j + bias[map[clamp(j - (start + i), -reach, reach) + reach]][head]) v_j over the keys j that query i of its sequence sees:
+ * j < k_lengths[b], and j <= q_start[b] + i with causal = 1, for i < q_lengths[b].  Query head h reads K/V head h / (n_head / n_kv_head).  A row that sees nothing, or lies
+ * behind its length, gets zeros (lse -inf) and passes no gradient on.  What hidden places hold, NaN and infinities among it, changes nothing.          */
+typedef struct {
+  int32_t dtype, batch, n_q, n_k, n_head, n_kv_head;
+  int32_t head_dim;                 /* a multiple of 8 up to 128                                      */
+  int32_t causal;
+  float   scale;                    /* > 0                                                            */
+  const int32_t* q_lengths;         /* [batch] or NULL: n_q (clamped to [0, n_q])                      */
+  const int32_t* k_lengths;         /* [batch] or NULL: n_k                                            */
+  const int32_t* q_start;           /* [batch] or NULL: 0, the key position of a sequence's first query */
+  const void*    bias;              /* [bias_buckets][n_head] or NULL: none                           */
+  const int32_t* bias_map;          /* [2 bias_reach + 1] buckets; one outside the table counts as NaN */
+  int32_t bias_buckets, bias_reach; /* bias_reach <= ZGR_MAX_REACH                                     */
+} zgr_attention;
+
+/* out: as q; lse: fp32 [batch][n_head][n_q], the natural logarithm of each row's sum of exponentials.           */
+size_t     zgr_attention_workspace(const zgr_attention* how);
+zgr_status zgr_attention_forward(const zgr_attention* how, const zgr_heads* q, const zgr_heads* k, const zgr_heads* v, const zgr_heads* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream);
+/* From dout and the forward pass's inputs and results: dq, dk, dv and dbias ([bias_buckets][n_head] in dtype: its terms come from probabilities and an `out` of that type; NULL: not wanted). */
+size_t     zgr_attention_backward_workspace(const zgr_attention* how);
+zgr_status zgr_attention_backward(const zgr_attention* how, const zgr_heads* dout, const zgr_heads* q, const zgr_heads* k, const zgr_heads* v, const zgr_heads* out, const float* lse,
+                                  const zgr_heads* dq, const zgr_heads* dk, const zgr_heads* dv, void* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* out = residual + keep (x + bias) / (1 - p), entry by entry of [rows, cols]; *_row: entries from a row to the next.  x and bias in x_dtype (bias [cols] or NULL), residual (or
+ * NULL) and out in stream_dtype; out may be residual, or x of the same type.  keep is a function of (seed, step, site, row, column) and stored nowhere: word c % 4 of
+ * Philox4x32-10 with key `seed` and counter (low and high word of (first_row + row) ceil(cols / 4) + c / 4, the high one with bit 31 set, site, step), at or above p 2^32 (rounded to the nearest
+ * whole number).  No perturbation draws from these counters, and both loss evaluations of a step that pass the same step get the same mask.  0 <= p < 1, step and first_row < 2^32.
+ * A dropped entry is zero whatever x holds there.                                                              */
+zgr_status zgr_dropout_add(int32_t rows, int32_t cols, int32_t x_dtype, const void* x, int64_t x_row, const void* bias, int32_t stream_dtype, const void* residual, int64_t residual_row, void* out,
+                           int64_t out_row, double p, uint64_t seed, uint64_t step, uint32_t site, uint64_t first_row, void* hip_stream);
+/* dx = keep dout / (1 - p) (dx may be dout where their types agree), dbias: fp32 [cols], its sums over rows, or NULL (then without a workspace).  The residual's gradient is dout. */
+size_t     zgr_dropout_add_backward_workspace(int32_t rows, int32_t cols);
+zgr_status zgr_dropout_add_backward(int32_t rows, int32_t cols, int32_t stream_dtype, const void* dout, int64_t dout_row, int32_t x_dtype, void* dx, int64_t dx_row, float* dbias, double p,
+                                    uint64_t seed, uint64_t step, uint32_t site, uint64_t first_row, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Client block of Algorithm 1 for round/step `step` (< 2^32): perturb all
  * tensors in place by +eps Z, evaluate L+, by -2 eps Z, evaluate L-, restore by
  * +eps Z, Z regenerated from (seed, step) in each pass.  Fills *out.  On

@@ -17,6 +17,7 @@ ZGR_ERR_WORKSPACE, ZGR_ERR_DEVICE, ZGR_ERR_NONFINITE, ZGR_ERR_STATE = 5, 6, 7, 8
 ZGR_F32, ZGR_BF16 = 0, 1
 ZGR_SCALE_UNIT, ZGR_SCALE_PAPER = 0, 1
 ZGR_MAX_BATCH = 8
+ZGR_MAX_REACH = 1024
 ZGR_ARCH_NONE, ZGR_ARCH_LINEAR_LSQ, ZGR_ARCH_DECODER_LM, ZGR_ARCH_ENCODER_CLS = -1, 0, 1, 2
 ZGR_K_PERTURB_TILE, ZGR_K_PERTURB_FLAT, ZGR_K_GEMM, ZGR_K_ATTN, ZGR_K_NORM, ZGR_K_EMBED, ZGR_K_LOSS, ZGR_K_COUNT = range(8)
 KERNEL_CLASS_NAMES = ("perturb_tile", "perturb_flat", "gemm", "attention", "norm", "embed", "loss")
@@ -47,6 +48,24 @@ class zgr_result(C.Structure):
     _fields_ = [("loss_plus", C.c_double), ("loss_minus", C.c_double), ("g", C.c_float)]
 
 
+class zgr_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class zgr_rotation(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("n_positions", C.c_int32), ("eps", C.c_float), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p),
+                ("table", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class zgr_attention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("n_q", C.c_int32), ("n_k", C.c_int32), ("n_head", C.c_int32), ("n_kv_head", C.c_int32), ("head_dim", C.c_int32),
+                ("causal", C.c_int32), ("scale", C.c_float), ("q_lengths", C.c_void_p), ("k_lengths", C.c_void_p), ("q_start", C.c_void_p), ("bias", C.c_void_p),
+                ("bias_map", C.c_void_p), ("bias_buckets", C.c_int32), ("bias_reach", C.c_int32)]
+
+
+_H = C.POINTER(zgr_heads)
+
 # every symbol include/zgr.h declares: name -> (restype, argtypes)
 SYMBOLS = {
     "zgr_workspace_bytes": (C.c_size_t, [C.POINTER(zgr_model), C.POINTER(zgr_tensor), C.c_int32, C.c_int32, C.c_int32]),
@@ -72,6 +91,19 @@ SYMBOLS = {
     "zgr_perturb": (C.c_int, [C.c_void_p, C.c_uint64, C.c_float]),
     "zgr_loss": (C.c_int, [C.c_void_p, C.POINTER(zgr_batch), C.POINTER(C.c_double)]),
     "zgr_lsq_loss_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
+    "zgr_norm_rotate": (C.c_int, [C.POINTER(zgr_rotation), _H, _H, _H, _H, C.c_void_p]),
+    "zgr_norm_rotate_backward_workspace": (C.c_size_t, [C.POINTER(zgr_rotation)]),
+    "zgr_norm_rotate_backward": (C.c_int, [C.POINTER(zgr_rotation), _H, _H, _H, _H, _H, _H, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zgr_relative_buckets": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]),
+    "zgr_attention_workspace": (C.c_size_t, [C.POINTER(zgr_attention)]),
+    "zgr_attention_forward": (C.c_int, [C.POINTER(zgr_attention), _H, _H, _H, _H, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zgr_attention_backward_workspace": (C.c_size_t, [C.POINTER(zgr_attention)]),
+    "zgr_attention_backward": (C.c_int, [C.POINTER(zgr_attention), _H, _H, _H, _H, _H, C.c_void_p, _H, _H, _H, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zgr_dropout_add": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_double,
+                                  C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint64, C.c_void_p]),
+    "zgr_dropout_add_backward_workspace": (C.c_size_t, [C.c_int32, C.c_int32]),
+    "zgr_dropout_add_backward": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_double,
+                                           C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint64, C.c_void_p, C.c_size_t, C.c_void_p]),
     "zgr_destroy": (None, [C.c_void_p]),
     "zgr_last_error": (C.c_char_p, [C.c_void_p]),
     "zgr_profile_enable": (C.c_int, [C.c_void_p, C.c_int32]),

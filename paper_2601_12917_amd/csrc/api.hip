@@ -7,6 +7,7 @@
 #include "forward.h"
 #include "internal.h"
 #include "product.h"
+#include "sublayer.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -116,6 +117,20 @@ zgr_status fail(zgr_ctx* c, zgr_status st, const char* fmt, ...) {
   if (c) c->err = buf; else g_init_error = buf;
   return st;
 }
+
+}  // namespace
+
+// the sublayer's operators have no context (sublayer_api.hip)
+zgr_status zgr::refuse(zgr_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(nullptr, st, "%s", buf);
+}
+
+namespace {
 
 #define HIP_TRY(ctx, expr)                                                                      \
   do {                                                                                          \

@@ -1,0 +1,188 @@
+// Dropout from a counter-based generator, with the bias in front of it and the residual sum behind it, and its gradient.  The mask is a function of (seed, step, site, row,
+// column) and never stored: the backward pass draws it again, and so may the second loss evaluation of a step or the edge server.
+// Philox4x32-10 as the perturbations have it, with bit 31 of the second counter word set, which their counters never reach: the same seed gives dropout and
+// perturbations different words.  One call makes the words of four consecutive columns of a row.
+// Bound by memory: 10 bytes an entry forward (bf16 onto an fp32 stream), 6 backward, against some 20 vector instructions an entry, which the loads hide.
+#include "rng.h"
+#include "sublayer.h"
+
+namespace zgr {
+
+namespace {
+
+constexpr uint32_t kDropoutWord = 0x80000000u;
+constexpr int kDropRun = 8;                       // entries of a lane: two calls, 16 bytes of bf16
+
+// keep[i] of the kDropRun columns from 4 call on of a row whose first call is row_call
+__device__ __forceinline__ void keep_run(const DropoutArgs& a, uint64_t q, bool (&keep)[kDropRun]) {
+#pragma unroll
+  for (int j = 0; j < kDropRun / 4; ++j) {
+    const uint64_t c = q + j;
+    const u32x4 w = philox4x32_10((uint32_t)c, (uint32_t)(c >> 32) | kDropoutWord, a.site, a.step, a.k0, a.k1);
+    keep[4 * j] = w.x >= a.threshold;
+    keep[4 * j + 1] = w.y >= a.threshold;
+    keep[4 * j + 2] = w.z >= a.threshold;
+    keep[4 * j + 3] = w.w >= a.threshold;
+  }
+}
+
+// n < kDropRun entries one by one
+template <typename T> __device__ __forceinline__ void load_some(const T* p, int n, float (&f)[kDropRun]) {
+#pragma unroll
+  for (int i = 0; i < kDropRun; ++i) f[i] = i < n ? as_float(p[i]) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void store_some(T* p, int n, const float (&f)[kDropRun]) {
+#pragma unroll
+  for (int i = 0; i < kDropRun; ++i) if (i < n) put_float(f[i], p + i);
+}
+
+// A block takes 256 runs one behind the other, over the ends of rows.
+template <typename T, typename S>
+__global__ void __launch_bounds__(256) dropout_add_kernel(DropoutArgs a) {
+  const uint32_t runs = (uint32_t)(a.cols + kDropRun - 1) / kDropRun;
+  const uint64_t base = (uint64_t)blockIdx.x * 256;
+  const uint64_t row0 = base / runs;
+  const uint32_t at = (uint32_t)(base - row0 * runs) + threadIdx.x;
+  const uint32_t down = at / runs, col = (at - down * runs) * kDropRun;
+  const uint64_t row = row0 + down;
+  if (row >= (uint64_t)a.rows) return;
+  const int n = min(kDropRun, a.cols - (int)col);
+  const T* x = (const T*)a.x + row * a.x_row + col;
+  const T* bias = a.bias ? (const T*)a.bias + col : nullptr;
+  const S* residual = a.residual ? (const S*)a.residual + row * a.residual_row + col : nullptr;
+  S* out = (S*)a.out + row * a.out_row + col;
+  float v[kDropRun], b[kDropRun] = {}, r[kDropRun] = {};
+  if (n == kDropRun) {
+    load_run(x, v);
+    if (bias) load_run(bias, b);
+    if (residual) load_run(residual, r);
+  } else {
+    load_some(x, n, v);
+    if (bias) load_some(bias, n, b);
+    if (residual) load_some(residual, n, r);
+  }
+  bool keep[kDropRun];
+  if (a.threshold) {
+    const uint64_t calls = ((uint32_t)a.cols + 3) / 4;
+    keep_run(a, (a.first_row + row) * calls + col / 4, keep);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kDropRun; ++i) keep[i] = true;
+  }
+#pragma unroll
+  for (int i = 0; i < kDropRun; ++i) v[i] = r[i] + (keep[i] ? (v[i] + b[i]) * a.scale : 0.f);
+  if (n == kDropRun) store_run(out, v);
+  else store_some(out, n, v);
+}
+
+// dx = keep dout scale and the sums of its columns.  A block takes `wide` runs of a row and 256 / wide rows at once, and every column sum meets its rows in one order: a thread's own,
+// then the threads of a column, then (launch_part_sums) the blocks.
+template <typename T, typename S>
+__global__ void __launch_bounds__(256) dropout_backward_kernel(DropoutArgs a, int wide, int rows_per_block) {
+  __shared__ float sums[256][kDropRun + 1];
+  const uint32_t runs = (uint32_t)(a.cols + kDropRun - 1) / kDropRun;
+  const int high = 256 / wide, tx = threadIdx.x % wide, ty = threadIdx.x / wide;
+  const uint32_t run = blockIdx.x * wide + tx, col = run * kDropRun;
+  const int64_t row_end = min((int64_t)a.rows, (int64_t)(blockIdx.y + 1) * rows_per_block);
+  const uint64_t calls = ((uint32_t)a.cols + 3) / 4;
+  const bool active = run < runs && ty < high;
+  const int n = active ? min(kDropRun, a.cols - (int)col) : 0;
+  float db[kDropRun] = {};
+  if (active) {
+    for (int64_t row = (int64_t)blockIdx.y * rows_per_block + ty; row < row_end; row += high) {
+      const S* dout = (const S*)a.out + row * a.out_row + col;
+      T* dx = (T*)a.x + row * a.x_row + col;
+      float v[kDropRun];
+      if (n == kDropRun) load_run(dout, v);
+      else load_some(dout, n, v);
+      bool keep[kDropRun];
+      if (a.threshold) keep_run(a, (a.first_row + row) * calls + col / 4, keep);
+      else
+#pragma unroll
+        for (int i = 0; i < kDropRun; ++i) keep[i] = true;
+#pragma unroll
+      for (int i = 0; i < kDropRun; ++i) {
+        v[i] = keep[i] ? v[i] * a.scale : 0.f;
+        db[i] += v[i];
+      }
+      if (n == kDropRun) store_run(dx, v);
+      else store_some(dx, n, v);
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int i = 0; i < kDropRun; ++i) sums[threadIdx.x][i] = db[i];
+  __syncthreads();
+  if (active && ty == 0) {
+    for (int y = 1; y < high; ++y)
+#pragma unroll
+      for (int i = 0; i < kDropRun; ++i) db[i] += sums[y * wide + tx][i];
+    store_some(a.part + (int64_t)blockIdx.y * a.cols + col, n, db);
+  }
+}
+
+__global__ void __launch_bounds__(1024) part_sums_kernel(const float* __restrict__ part, int parts, int n, float* __restrict__ out) {
+  __shared__ float sums[32][33];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+  float v = 0.f;
+  if (c < n) {
+#pragma unroll 4
+    for (int p = ty; p < parts; p += 32) v += part[(int64_t)p * n + c];
+  }
+  sums[ty][tx] = v;
+  __syncthreads();
+  if (ty == 0 && c < n) {
+    for (int y = 1; y < 32; ++y) v += sums[y][tx];
+    out[c] = v;
+  }
+}
+
+struct Strips { int wide, strips, parts, rows_per_block; };
+// Runs of a row are spread evenly over strips of at most 256 of them; the rows over as many blocks as make some 1024 in all, with 8 rows at least for each thread.
+Strips strips_of(int rows, int cols) {
+  Strips t;
+  const int runs = (cols + kDropRun - 1) / kDropRun;
+  t.strips = (runs + 255) / 256;
+  t.wide = (runs + t.strips - 1) / t.strips;
+  const int high = 256 / t.wide;
+  int parts = (1024 + t.strips - 1) / t.strips;
+  parts = (int)((int64_t)rows < (int64_t)parts * 8 * high ? ((int64_t)rows + 8 * high - 1) / (8 * high) : parts);
+  t.rows_per_block = (int)(((int64_t)rows + parts - 1) / parts);
+  t.parts = (rows + t.rows_per_block - 1) / t.rows_per_block;
+  return t;
+}
+
+}  // namespace
+
+hipError_t launch_part_sums(const float* part, int parts, int n, float* out, hipStream_t s) {
+  hipLaunchKernelGGL(part_sums_kernel, dim3((n + 31) / 32), dim3(1024), 0, s, part, parts, n, out);
+  return hipGetLastError();
+}
+
+int dropout_parts(int rows, int cols) { return strips_of(rows, cols).parts; }
+
+hipError_t launch_dropout_add(const DropoutArgs& a, hipStream_t s) {
+  const uint64_t runs = (uint64_t)((a.cols + kDropRun - 1) / kDropRun) * (uint64_t)a.rows;
+  const dim3 grid((unsigned)((runs + 255) / 256));
+  switch (2 * a.x_dtype + a.stream_dtype) {
+    case 0: hipLaunchKernelGGL((dropout_add_kernel<float, float>), grid, dim3(256), 0, s, a); break;
+    case 1: hipLaunchKernelGGL((dropout_add_kernel<float, bf16_bits>), grid, dim3(256), 0, s, a); break;
+    case 2: hipLaunchKernelGGL((dropout_add_kernel<bf16_bits, float>), grid, dim3(256), 0, s, a); break;
+    default: hipLaunchKernelGGL((dropout_add_kernel<bf16_bits, bf16_bits>), grid, dim3(256), 0, s, a); break;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_dropout_add_backward(const DropoutArgs& a, hipStream_t s) {
+  const Strips t = strips_of(a.rows, a.cols);
+  const dim3 grid(t.strips, t.parts);
+  switch (2 * a.x_dtype + a.stream_dtype) {
+    case 0: hipLaunchKernelGGL((dropout_backward_kernel<float, float>), grid, dim3(256), 0, s, a, t.wide, t.rows_per_block); break;
+    case 1: hipLaunchKernelGGL((dropout_backward_kernel<float, bf16_bits>), grid, dim3(256), 0, s, a, t.wide, t.rows_per_block); break;
+    case 2: hipLaunchKernelGGL((dropout_backward_kernel<bf16_bits, float>), grid, dim3(256), 0, s, a, t.wide, t.rows_per_block); break;
+    default: hipLaunchKernelGGL((dropout_backward_kernel<bf16_bits, bf16_bits>), grid, dim3(256), 0, s, a, t.wide, t.rows_per_block); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace zgr

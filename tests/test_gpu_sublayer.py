@@ -1,0 +1,456 @@
+"""The attention sublayer's operators against their definitions in 64 bits, at the sizes, masks, strides and types where they can go wrong."""
+import math
+
+import pytest
+import torch
+
+from tests import sublayer_reference as R
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2601_12917_amd import sublayer
+    return sublayer
+
+
+def _normal(g, *shape, dtype=F32, std=1.0, mean=0.0):
+    return (torch.randn(*shape, generator=g) * std + mean).to(dtype).cuda()
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+# ------------------------------------------------------------------------------------------------ attention
+def _inputs(dtype, b, n_q, n_k, heads, kv_heads, dim, buckets=0, reach=0, causal=False, seed=0):
+    g = _gen(seed)
+    q, k, v, dout = (_normal(g, b, n, h, dim, dtype=dtype) for n, h in ((n_q, heads), (n_k, kv_heads), (n_k, kv_heads), (n_q, heads)))
+    how = dict(causal=causal)
+    if buckets:
+        from paper_2601_12917_amd import sublayer as S
+        how.update(bias=_normal(g, buckets, heads, dtype=dtype), bias_map=S.relative_buckets(buckets, reach, causal))
+    return q, k, v, dout, how
+
+
+def _compare(S, q, k, v, dout, how, grads=True):
+    out, lse = S.attention(q, k, v, **how)
+    if not grads:
+        for n, a, w in zip(("out", "lse"), (out, lse), R.attention(q, k, v, **how)):
+            R.check(a, w, n)
+        return out, lse
+    got = (out, lse, *S.attention_backward(dout, q, k, v, out, lse, **how))
+    *want, terms = R.attention(q, k, v, **how, dout=dout)
+    for n, a, w in zip(("out", "lse", "dq", "dk", "dv", "dbias"), got, want):
+        if w is None:
+            assert a is None, n
+        else:
+            R.check(a, w, n, terms=terms.get(n))
+    return got
+
+
+@TYPES
+@pytest.mark.parametrize("causal", [False, True], ids=["both", "causal"])
+@pytest.mark.parametrize("n_q,n_k", [(1, 1), (2, 3), (31, 31), (32, 32), (33, 33), (64, 65), (65, 64), (1, 130), (127, 129), (130, 1), (200, 200)])
+def test_lengths_at_the_edges_of_tiles(S, dtype, causal, n_q, n_k):
+    _compare(S, *_inputs(dtype, 2, n_q, n_k, 2, 2, 64, 8, 20, causal, seed=n_q * 1000 + n_k))
+
+
+@TYPES
+@pytest.mark.parametrize("dim", [8, 16, 24, 32, 40, 64, 72, 96, 120, 128])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (6, 2), (4, 1)])
+def test_head_sizes_and_shared_heads(S, dtype, dim, heads, kv_heads):
+    _compare(S, *_inputs(dtype, 2, 70, 70, heads, kv_heads, dim, 16, 32, True, seed=dim + heads))
+
+
+@TYPES
+@pytest.mark.parametrize("buckets,reach", [(1, 0), (2, 1), (5, 7), (32, 31), (32, 32), (32, 33), (33, 100), (64, 600), (8, 1024)])
+@pytest.mark.parametrize("causal", [False, True], ids=["both", "causal"])
+def test_bias_reaches(S, dtype, buckets, reach, causal):
+    buckets = max(buckets, 1 if causal else 2)
+    _compare(S, *_inputs(dtype, 1, 190, 190, 2, 1, 32, buckets, reach, causal, seed=reach))
+
+
+@TYPES
+def test_without_a_bias_and_with_a_scale(S, dtype):
+    q, k, v, dout, how = _inputs(dtype, 2, 75, 90, 2, 2, 40, seed=3)
+    _compare(S, q, k, v, dout, dict(how, scale=0.5))
+    _compare(S, q, k, v, dout, dict(how, scale=0.01, causal=True))
+
+
+@TYPES
+@pytest.mark.parametrize("causal", [False, True], ids=["both", "causal"])
+def test_lengths_and_starts_leave_rows_empty(S, dtype, causal):
+    """Lengths of 0 and 1, lengths inside a tile and past the tensor, first queries in front of the first key and behind the last."""
+    q, k, v, dout, how = _inputs(dtype, 8, 70, 100, 2, 1, 64, 8, 20, causal, seed=9)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    how.update(q_lengths=ints(70, 0, 1, 33, 64, 70, -5, 1000), k_lengths=ints(100, 40, 0, 1, 65, 100, 100, 99), q_start=ints(30, 0, 5, -3, -40, -200, 0, 1 << 30))
+    out, lse = _compare(S, q, k, v, dout, how)[:2]
+    assert torch.all(out[1] == 0) and torch.all(lse[2] == -math.inf) and torch.all(out[2] == 0) and torch.all(out[7, :, :, 0].isfinite())
+
+
+@TYPES
+def test_nothing_to_attend(S, dtype):
+    """No keys, no queries, no sequences: zeros, and nothing else happens."""
+    q, k, v, dout, how = _inputs(dtype, 2, 5, 7, 2, 2, 32, 4, 3, False, seed=1)
+    none = k[:, :0]
+    out, lse = S.attention(q, none, none, **how)
+    assert torch.all(out == 0) and torch.all(lse == -math.inf)
+    dq, dk, dv, db = S.attention_backward(dout, q, none, none, out, lse, **how)
+    assert torch.all(dq == 0) and torch.all(db == 0) and dk.shape == none.shape
+    out, lse = S.attention(q[:, :0], k, v, **how)
+    dq, dk, dv, db = S.attention_backward(dout[:, :0], q[:, :0], k, v, out, lse, **how)
+    assert out.numel() == 0 and torch.all(dk == 0) and torch.all(dv == 0) and torch.all(db == 0)
+    out, lse = S.attention(q[:0], k[:0], v[:0], **how)
+    assert out.numel() == 0 and torch.all(S.attention_backward(dout[:0], q[:0], k[:0], v[:0], out, lse, **how)[3] == 0)
+
+
+@TYPES
+@pytest.mark.parametrize("layout", ["projection", "cache", "mixed"])
+def test_strides_and_orders(S, dtype, layout):
+    b, n, heads, kv, dim = 3, 45, 4, 2, 24
+    g = _gen(4)
+    if layout == "projection":
+        qkv = _normal(g, b, n, (heads + 2 * kv) * dim, dtype=dtype)
+        q, k, v = (t.unflatten(-1, (-1, dim)) for t in qkv.split([heads * dim, kv * dim, kv * dim], -1))
+    elif layout == "cache":
+        q = _normal(g, heads, b, n, dim, dtype=dtype).permute(1, 2, 0, 3)
+        k, v = (_normal(g, b, kv, n + 9, dim, dtype=dtype)[:, :, :n].transpose(1, 2) for _ in range(2))
+    else:
+        q = _normal(g, n, b, heads, dim + 8, dtype=dtype).transpose(0, 1)[..., :dim]
+        k, v = _normal(g, n, kv, b, dim, dtype=dtype).permute(2, 0, 1, 3), _normal(g, b, n, kv, 2 * dim, dtype=dtype)[..., dim:]
+    dout = _normal(g, b, heads, n, dim, dtype=dtype).transpose(1, 2)
+    how = dict(causal=True, bias=_normal(g, 6, heads, dtype=dtype), bias_map=S.relative_buckets(6, 9, True))
+    _compare(S, q, k, v, dout, how)
+    where = torch.full((b, n, heads, dim + 8), 7.0, dtype=dtype, device="cuda")
+    out, _ = S.attention(q, k, v, **how, out=where[..., :dim])
+    assert out.data_ptr() == where.data_ptr() and torch.all(where[..., dim:] == 7)
+    R.check(out, R.attention(q, k, v, **how)[0], "out")
+
+
+@TYPES
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_what_lies_behind_the_lengths_is_never_read(S, dtype, value):
+    """The same bits whatever q, k, v and dout hold there."""
+    q, k, v, dout, how = _inputs(dtype, 3, 70, 70, 2, 1, 64, 8, 20, False, seed=12)
+    lengths = torch.tensor([70, 37, 1], dtype=torch.int32, device="cuda")
+    how.update(q_lengths=lengths, k_lengths=lengths)
+    out, lse = S.attention(q, k, v, **how)
+    want = (out, lse, *S.attention_backward(dout, q, k, v, out, lse, **how))
+    for n, length in enumerate(lengths.tolist()):
+        for t in (q, k, v, dout):
+            t[n, length:] = value
+    out, lse = S.attention(q, k, v, **how)
+    got = (out, lse, *S.attention_backward(dout, q, k, v, out, lse, **how))
+    for a, w in zip(got, want):
+        assert torch.equal(a, w)
+
+
+@TYPES
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("at", [1, 40, 63, 99])
+def test_a_query_does_not_see_what_a_later_position_holds(S, dtype, dim, at):
+    """Causal mask: earlier rows and their gradients are what they were; a later row has NaN or infinity where its sum has."""
+    q, k, v, dout, how = _inputs(dtype, 1, 100, 100, 2, 1, dim, 8, 20, True, seed=13)
+    want = R.attention(q, k, v, **how, dout=dout)
+    v[0, at, 0, 3], k[0, at, 0, 1] = math.inf, math.nan
+    out, lse = S.attention(q, k, v, **how)
+    R.check(out[:, :at], want[0][:, :at], "out")
+    R.check(lse[:, :, :at], want[1][:, :, :at], "lse")
+    assert out[:, at:].isnan().all()
+    dq = S.attention_backward(dout, q, k, v, out, lse, **how)[0]
+    R.check(dq[:, :at], want[2][:, :at], "dq", terms=want[6]["dq"][:, :at])
+    k[0, at, 0, 1] = 0.5                                                     # an infinite value alone: infinite in its own entry of the rows that see it
+    out, _ = S.attention(q, k, v, **how)
+    assert (out[:, at:, :, 3] == math.inf).all() and out[..., :3].isfinite().all() and out[..., 4:].isfinite().all() and out[:, :at].isfinite().all()
+
+
+@TYPES
+def test_a_later_query_that_is_not_finite_leaves_keys_it_does_not_see(S, dtype):
+    """Queries 20 .. see keys from 0 on; the first query sees none of the keys behind it, whatever its row holds."""
+    q, k, v, dout, how = _inputs(dtype, 1, 60, 60, 1, 1, 64, 8, 20, True, seed=14)
+    want = R.attention(q[:, 1:], k, v, dout=dout[:, 1:], **dict(how, q_start=torch.tensor([1])))
+    dout[0, 0] = math.nan
+    out, lse = S.attention(q, k, v, **how)
+    _, dk, dv, _ = S.attention_backward(dout, q, k, v, out, lse, **how)
+    assert dv[0, 0].isnan().all()
+    R.check(dk[:, 1:], want[3][:, 1:], "dk", terms=want[6]["dk"][:, 1:])
+    R.check(dv[:, 1:], want[4][:, 1:], "dv")
+
+
+@TYPES
+@pytest.mark.parametrize("low", [-math.inf, None], ids=["-inf", "lowest"])
+def test_buckets_that_hide(S, dtype, low):
+    """A bias of -infinity, and of the type's lowest value, hides a bucket's keys; a row all of whose keys it hides is the mean of them only where the value is finite."""
+    q, k, v, dout, how = _inputs(dtype, 1, 80, 80, 2, 2, 32, 4, 3, False, seed=5)
+    how["bias"][1] = torch.finfo(dtype).min if low is None else low
+    _compare(S, q, k, v, dout, how, grads=False)
+    out, lse = S.attention(q, k, v, **how)
+    assert all(t.isfinite().all() for t in S.attention_backward(dout, q, k, v, out, lse, **how))
+    how["bias"][:] = low if low is not None else -3.0e38
+    out, lse = S.attention(q, k, v, **how)
+    if low is not None:
+        assert (out == 0).all() and (lse == -math.inf).all()
+        assert all((t == 0).all() for t in S.attention_backward(dout, q, k, v, out, lse, **how))
+    else:
+        assert out.isfinite().all()
+
+
+def test_a_bucket_outside_the_table_is_nan(S):
+    q, k, v, dout, how = _inputs(F32, 1, 10, 10, 1, 1, 32, 4, 3, True, seed=5)
+    how["bias_map"][2] = 4                                                   # one position before the query
+    out, _ = S.attention(q, k, v, **how)
+    assert out[0, 0].isfinite().all() and out[0, 1:].isnan().all()
+
+
+@TYPES
+def test_large_scores(S, dtype):
+    """Scores of some thousands: the running maximum carries them."""
+    q, k, v, dout, how = _inputs(dtype, 1, 96, 96, 1, 1, 64, 4, 10, True, seed=6)
+    q, k = (q.double() * 30).to(dtype), (k.double() * 30).to(dtype)
+    out, lse = S.attention(q, k, v, **how)
+    want = R.attention(q, k, v, **how)
+    assert float((lse.cpu().double() - want[1]).abs().max()) <= 64 * 2.0 ** -24 * float(want[1].abs().max())
+    assert float((out.cpu().double() - want[0]).norm() / want[0].norm()) <= (2.0 ** -7 if dtype is BF16 else 1e-2)      # fp32 scores of 2^13 are 2^-11 apart
+
+
+@TYPES
+@pytest.mark.parametrize("n_q,heads,kv_heads,dim,n_k", [(1, 8, 1, 128, 3000), (1, 4, 4, 64, 1), (1, 2, 2, 32, 257), (3, 8, 2, 128, 1025), (20, 4, 1, 64, 600), (1, 96, 1, 64, 700), (40, 2, 1, 40, 2100)])
+def test_few_queries_over_a_long_cache(S, dtype, n_q, heads, kv_heads, dim, n_k):
+    q, k, v, dout, how = _inputs(dtype, 3, n_q, n_k, heads, kv_heads, dim, 32, 128, True, seed=n_k)
+    k, v = (t.transpose(1, 2).contiguous().transpose(1, 2) for t in (k, v))
+    lengths = torch.tensor([n_k, max(1, n_k // 3), 1], dtype=torch.int32, device="cuda")
+    how.update(k_lengths=lengths, q_start=lengths - n_q)
+    _compare(S, q, k, v, dout, how, grads=False)
+    _compare(S, q, k, v, dout, dict(how, causal=False), grads=False)
+
+
+@TYPES
+def test_one_token_over_hidden_nan(S, dtype):
+    q, k, v, dout, how = _inputs(dtype, 2, 1, 900, 4, 1, 64, 32, 128, True, seed=2)
+    lengths = torch.tensor([700, 0], dtype=torch.int32, device="cuda")
+    how.update(k_lengths=lengths, q_start=torch.tensor([640, 5], dtype=torch.int32, device="cuda"))
+    want = R.attention(q, k, v, **how)
+    k[:, 700:], v[:, 641:], k[1], v[1] = math.nan, math.nan, math.nan, math.inf
+    out, lse = S.attention(q, k, v, **how)
+    R.check(out, want[0], "out")
+    R.check(lse, want[1], "lse")
+
+
+@TYPES
+def test_offsets_past_32_bits(S, dtype):
+    """A cache whose rows lie 2^19 entries apart: 2^32 entries and more from the first to the last."""
+    n_k, step = 9000, 1 << 19
+    if torch.cuda.mem_get_info()[0] < 2 * n_k * step * dtype.itemsize // 2:
+        pytest.skip("no room")
+    cache = torch.empty(n_k * step, dtype=dtype, device="cuda")
+    k = cache.view(1, n_k, 1, step)[..., :32]
+    v = cache.view(1, n_k, 1, step)[..., 64:96]
+    g = _gen(8)
+    k.copy_(_normal(g, 1, n_k, 1, 32, dtype=dtype))
+    v.copy_(_normal(g, 1, n_k, 1, 32, dtype=dtype))
+    q, dout = _normal(g, 1, 2, 1, 32, dtype=dtype), _normal(g, 1, 2, 1, 32, dtype=dtype)
+    how = dict(causal=True, q_start=torch.tensor([n_k - 2], dtype=torch.int32, device="cuda"))
+    _compare(S, q, k, v, dout, how)
+
+
+@TYPES
+def test_two_runs_give_the_same_bits(S, dtype):
+    q, k, v, dout, how = _inputs(dtype, 3, 300, 300, 4, 2, 64, 32, 128, True, seed=7)
+
+    def once():
+        out, lse = S.attention(q, k, v, **how)
+        return (out, lse, *S.attention_backward(dout, q, k, v, out, lse, **how))
+    first = once()
+    for _ in range(3):
+        for a, b in zip(first, once()):
+            assert torch.equal(a, b)
+
+
+def test_on_another_stream(S):
+    """The calls go to the current stream: inputs that it makes are ready, and results are its own."""
+    q, k, v, dout, how = _inputs(BF16, 2, 200, 200, 4, 2, 64, 32, 64, True, seed=7)
+    want = S.attention(q, k, v, **how)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        late = q.clone()
+        for _ in range(50):
+            late = late * 1.0
+        got = S.attention(late, k, v, **how)[0]
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+
+
+def test_gradients_against_differences(S):
+    """fp32: the change of sum(out w) along a direction in q, k, v and the bias together, by central differences of the 64-bit definition and of the operator itself."""
+    q, k, v, w, how = _inputs(F32, 2, 50, 50, 4, 2, 32, 8, 20, True, seed=21)
+    g = _gen(22)
+    steps = [_normal(g, *t.shape) for t in (q, k, v, how["bias"])]
+    out, lse = S.attention(q, k, v, **how)
+    grads = S.attention_backward(w, q, k, v, out, lse, **how)
+    want = sum(float((a.double() * b.double()).sum()) for a, b in zip(grads, steps))
+
+    def at(h):
+        moved = [(t.double() + h * d.double()).float() for t, d in zip((q, k, v, how["bias"]), steps)]
+        return float((S.attention(*moved[:3], **dict(how, bias=moved[3]))[0].double() * w.double()).sum())
+    h = 2.0 ** -8                                                            # the error is of order h^2 = 1.5e-5, the rounding 1e-6 / h
+    scale = math.sqrt(sum(float((a.double() ** 2).sum()) for a in grads))
+    assert abs((at(h) - at(-h)) / (2 * h) - want) <= 2e-3 * scale
+
+
+# ------------------------------------------------------------------------------------------------ norms and rotation
+@TYPES
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "pairs"])
+@pytest.mark.parametrize("dim,rot", [(8, 8), (16, 8), (24, 24), (32, 32), (64, 16), (64, 64), (80, 40), (96, 96), (128, 128), (128, 0), (200, 104), (256, 256)])
+def test_norm_rotate(S, dtype, interleaved, dim, rot):
+    g = _gen(dim * 3 + rot)
+    rows, heads, kv = 37, 5, 3
+    qkv = _normal(g, rows, (heads + 2 * kv) * dim, dtype=dtype)
+    q, k = qkv[:, :heads * dim].view(rows, heads, dim), qkv[:, heads * dim:(heads + kv) * dim].view(rows, kv, dim)
+    q[3], k[4, 1] = 0, 0                                                     # rows of zeros
+    gq, gk = _normal(g, dim, dtype=dtype, std=0.1, mean=1.0), _normal(g, dim, dtype=dtype, std=0.1, mean=1.0)
+    table = S.rotation_table(50, rot) if rot else None
+    at = torch.randint(0, 50, (rows,), generator=g, dtype=torch.int32).cuda()
+    dzq, dzk = _normal(g, rows, heads, dim, dtype=dtype), _normal(g, rows, kv, dim, dtype=dtype)
+    zq, zk = S.norm_rotate(q, k, gq, gk, table, at, interleaved=interleaved)
+    grads = S.norm_rotate_backward(dzq, dzk, q, k, gq, gk, table, at, interleaved=interleaved)
+    leaves = [t.detach().cpu().double().requires_grad_(True) for t in (q, k, gq, gk)]
+    cpu = (None, None) if table is None else (table.cpu(), at.cpu())
+    wq, wk = (R.rotate(x, gain, *cpu, interleaved=interleaved) for x, gain in ((leaves[0], leaves[2]), (leaves[1], leaves[3])))
+    R.check(zq, wq, "q")
+    R.check(zk, wk, "k")
+    want = torch.autograd.grad([wq, wk], leaves, [dzq.cpu().double(), dzk.cpu().double()])
+    for n, a, w in zip(("dq", "dk", "dq_gain", "dk_gain"), grads, want):
+        # a row of zeros has 1 / sqrt(eps) = 1000 times the others' gradient
+        R.check(a, w, n)
+    assert all(torch.equal(a, b) for a, b in zip(grads, S.norm_rotate_backward(dzq, dzk, q, k, gq, gk, table, at, interleaved=interleaved)))
+
+
+@TYPES
+@pytest.mark.parametrize("rows", [0, 1, 2, 3, 700, 5000])
+@pytest.mark.parametrize("heads,kv", [(1, 0), (0, 1), (32, 8), (3, 1)])
+def test_norm_rotate_rows_and_heads(S, dtype, rows, heads, kv):
+    g = _gen(rows + heads)
+    dim = 64
+    q = _normal(g, rows, heads, dim, dtype=dtype) if heads else None
+    k = _normal(g, kv, rows, dim, dtype=dtype).transpose(0, 1) if kv else None
+    gain, table = _normal(g, dim, dtype=dtype), S.rotation_table(100, dim)
+    at = torch.randint(0, 100, (rows,), generator=g, dtype=torch.int32).cuda()
+    z = S.norm_rotate(q, k, gain if heads else None, None, table, at)
+    d = S.norm_rotate_backward(*z, q, k, gain if heads else None, None, table, at)
+    for x, gn, zz, dd, dg in ((q, gain, z[0], d[0], d[2]), (k, None, z[1], d[1], d[3])):
+        if x is None:
+            assert zz is None and dd is None
+            continue
+        leaf, gl = x.cpu().double().requires_grad_(True), None if gn is None else gn.cpu().double().requires_grad_(True)
+        want = R.rotate(leaf, gl, table.cpu(), at.cpu())
+        R.check(zz, want, "z")
+        if rows:
+            grads = torch.autograd.grad(want, [leaf] if gl is None else [leaf, gl], zz.cpu().double())
+            R.check(dd, grads[0], "dx")
+            if gl is not None:
+                R.check(dg, grads[1], "dgain")
+        elif gn is not None:
+            assert (dg == 0).all()
+
+
+@TYPES
+def test_norm_rotate_in_place_and_positions_outside_the_table(S, dtype):
+    g = _gen(1)
+    q, k = _normal(g, 9, 4, 64, dtype=dtype), _normal(g, 9, 2, 64, dtype=dtype)
+    gq, gk, table = _normal(g, 64, dtype=dtype), _normal(g, 64, dtype=dtype), S.rotation_table(10, 32)
+    at = torch.tensor([0, 9, 10, -1, 5, 2 ** 31 - 1, -2 ** 31, 3, 4], dtype=torch.int32, device="cuda")
+    z = S.norm_rotate(q, k, gq, gk, table, at)
+    good = [0, 1, 4, 7, 8]
+    for zz, x, gain in ((z[0], q, gq), (z[1], k, gk)):
+        R.check(zz[good], R.rotate(x.cpu()[good], gain.cpu(), table.cpu(), at.cpu()[good]), "z")
+        bad = [i for i in range(9) if i not in good]
+        assert zz[bad][..., :32].isnan().all() and zz[bad][..., 32:].isfinite().all()
+    q2, k2 = q.clone(), k.clone()
+    S.norm_rotate(q2, k2, gq, gk, table, at, q_out=q2, k_out=k2)
+    assert torch.equal(q2[good], z[0][good]) and torch.equal(k2[good], z[1][good])
+
+
+def test_norm_rotate_gradients_against_differences(S):
+    g = _gen(30)
+    q, gain, table, w = _normal(g, 20, 3, 32), _normal(g, 32, mean=1.0, std=0.1), S.rotation_table(40, 16), _normal(g, 20, 3, 32)
+    at = torch.arange(20, dtype=torch.int32, device="cuda")
+    dq, _, dg, _ = S.norm_rotate_backward(w, None, q, None, gain, None, table, at)
+    steps = [_normal(g, *t.shape) for t in (q, gain)]
+    want = sum(float((a.double() * b.double()).sum()) for a, b in zip((dq, dg), steps))
+
+    def value(h):
+        return float((S.norm_rotate(q + h * steps[0], None, gain + h * steps[1], None, table, at)[0].double() * w.double()).sum())
+    h = 2.0 ** -8
+    scale = math.sqrt(sum(float((a.double() ** 2).sum()) for a in (dq, dg)))
+    assert abs((value(h) - value(-h)) / (2 * h) - want) <= 2e-3 * scale
+
+
+# ------------------------------------------------------------------------------------------------ dropout
+@pytest.mark.parametrize("stream", [F32, BF16], ids=["f32 stream", "bf16 stream"])
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 8), (33, 9), (64, 100), (7, 2051), (300, 768), (2, 5003), (1000, 3)])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.75])
+def test_dropout_add(S, dtype, stream, rows, cols, p):
+    g = _gen(rows * cols)
+    x, bias, res, dout = _normal(g, rows, cols, dtype=dtype), _normal(g, cols, dtype=dtype), _normal(g, rows, cols, dtype=stream), _normal(g, rows, cols, dtype=stream)
+    key = (p, 0x123456789ABCDEF0 + rows, 77, 3)
+    keep = R.keep_mask(rows, cols, *key)
+    out = S.dropout_add(x, bias, res, *key)
+    want = res.cpu().double() + torch.where(keep, (x.cpu().double() + bias.cpu().double()) / (1 - p), 0.0)
+    R.check(out, want, "out")
+    assert torch.equal(out.cpu()[~keep], res.cpu()[~keep])
+    dx, db = S.dropout_add_backward(dout, dtype, *key)
+    wdx = torch.where(keep, dout.cpu().double() / (1 - p), 0.0)
+    R.check(dx, wdx, "dx")
+    assert torch.equal(dx.cpu() == 0, (wdx == 0))
+    R.check(db, wdx.sum(0), "dbias")
+    assert torch.equal(db, S.dropout_add_backward(dout, dtype, *key)[1])
+    assert S.dropout_add_backward(dout, dtype, *key, want_bias=False)[1] is None
+    alone = S.dropout_add(x, None, None, *key)
+    assert alone.dtype is dtype and torch.equal(alone.cpu() != 0, keep & (x.cpu() != 0))
+
+
+@TYPES
+def test_dropout_views_rows_and_hidden_values(S, dtype):
+    """Rows of a wider tensor, off the alignment of wide loads; parts of a batch under first_row; dropped entries that are not finite; in place."""
+    g = _gen(2)
+    wide = _normal(g, 41, 131, dtype=dtype)
+    x, key = wide[:, 3:120], (0.3, 99, 5, 8)
+    keep = R.keep_mask(41, 117, *key).cuda()
+    x[~keep] = math.nan
+    res = _normal(g, 41, 140)[:, 1:118]
+    out = S.dropout_add(x, None, res, *key)
+    assert out.isfinite().all()
+    R.check(out, res.cpu().double() + torch.where(keep.cpu(), x.cpu().double() / 0.7, 0.0), "out")
+    parts = [S.dropout_add(x[a:b], None, res[a:b], *key, first_row=a) for a, b in ((0, 17), (17, 18), (18, 41))]
+    assert torch.equal(torch.cat(parts), out)
+    big = (1 << 32) - 41
+    assert torch.equal(S.dropout_add(x.nan_to_num(1.0), None, None, *key, first_row=big) != 0, R.keep_mask(41, 117, *key, first_row=big).cuda() & (x.nan_to_num(1.0) != 0))
+    S.dropout_add(x, None, res, *key, out=res)
+    assert torch.equal(res, out)
+    assert S.dropout_add(x[:0], None, res[:0], *key).shape == (0, 117)
+    dx, db = S.dropout_add_backward(res[:0], dtype, *key)
+    assert dx.shape == (0, 117) and (db == 0).all()
+
+
+def test_dropout_keeps_its_share_and_repeats_nothing(S):
+    """1 - p of 2^24 entries within five standard deviations; sites, steps and seeds give other masks; no word is one of a perturbation's."""
+    from paper_2601_12917_amd.session import debug_philox
+    import numpy as np
+    one = torch.ones(4096, 4096, device="cuda")
+    masks = [S.dropout_add(one, None, None, 0.25, *key) != 0 for key in ((1, 0, 0), (1, 0, 1), (1, 1, 0), (2, 0, 0))]
+    for m in masks:
+        assert abs(float(m.float().double().mean()) - 0.75) <= 5 * math.sqrt(0.25 * 0.75 / 2 ** 24)
+    for i, a in enumerate(masks):
+        for b in masks[:i]:
+            assert abs(float((a == b).float().double().mean()) - 0.625) <= 5 * math.sqrt(0.625 * 0.375 / 2 ** 24)
+    ctr = np.array([[0, 1 << 31, 0, 0], [0, 0, 0, 0]], dtype=np.uint32)
+    w = debug_philox(ctr, (1, 0))
+    assert (w[0] != w[1]).all()
+    assert [bool(v) for v in masks[0][0, :4]] == [int(v) >= 1 << 30 for v in w[0]]
