@@ -10,6 +10,9 @@
 // So p and ds go from the accumulators of one product into the operand of the next without leaving the lane, and sums over keys are sums over a lane's registers and one exchange.
 // bf16: v_mfma_f32_32x32x16_bf16, the second kind reads columns of LDS with ds_read_b64_tr_b16.  fp32: v_mfma_f32_32x32x2_f32.
 #include "sublayer.h"
+#include "wave.h"
+
+#include <type_traits>
 
 namespace zgr {
 
@@ -23,18 +26,16 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 constexpr int kBiasPad = 64;              // places beyond reach on either side that a tile with a key within reach can touch: look-ups need no clamp
 __device__ const u32x4_t kZeros[1] = {};
 
-// How the 16-byte pieces of a tile's rows lie in LDS: piece c of row r in place c ^ turn(r).  16 rows' same piece (the first kind of product) and four rows' 64 bytes (the
-// second) then lie in 64 different banks.
+// How the 16-byte pieces of a tile's rows lie in LDS: piece c of row r in place c ^ turn(r).  bf16: 16 rows' same piece (the first kind of product) and four rows' 64 bytes (the
+// second) then lie in 64 different banks.  fp32: turn looks at r % 8 alone, so that the second kind's addresses are four registers and immediates (with the other bits of r it took
+// 64 registers, and kernels that spilled).
 template <typename T, int DH> __device__ __forceinline__ int turn_of(int r) {
   constexpr int pieces = DH * (int)sizeof(T) / 16;
   if constexpr (sizeof(T) == 2) {
     if constexpr (pieces == 4) return (r >> 2) & 3;
     else if constexpr (pieces == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
     else return ((r & 3) << 2) | ((r >> 2) & 3);
-  } else {
-    if constexpr (pieces == 8) return (r >> 1) & 7;
-    else return (((r >> 2) & 1) << 3) | ((r & 3) << 1) | ((r >> 3) & 1);
-  }
+  } else return r & 7;
 }
 
 // A row of DH entries in the registers of two lanes (the halves of a wave), as the first kind of product takes it.
@@ -72,6 +73,29 @@ __device__ __forceinline__ float max_of_halves(float v) {
   const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
+// The sums of a tile along its diagonals, lane - row = t: in lane t, and 64 + t for t < 0 (-31 <= t <= 31).  The halves of each register, which hold rows four apart, become vectors of
+// 32 lanes and 32 zeros; a rotation of the wave by one lane is part of an addition, and by four, seven times, an exchange.  (Adding the 16 registers to places in LDS takes the
+// LDS unit a cycle a lane and more, as an atomic: it was 110 of 143 us of dq for 16 x 256 tokens, 32 heads.)
+__device__ __forceinline__ float diagonal_sums(const float (&x)[16], int lane) {
+  float total = 0.f;
+#pragma unroll
+  for (int c = 3; c >= 0; --c) {
+    u32x2_t u[4];                                           // rows 8 c + i, and + 4
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[4 * c + i]), 0u, false, false);
+      u[i] = u32x2_t{w[0], w[1]};
+    }
+#pragma unroll
+    for (int h = 1; h >= 0; --h) {
+      float acc = __uint_as_float(u[3][h]);
+#pragma unroll
+      for (int i = 2; i >= 0; --i) acc = __uint_as_float(u[i][h]) + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(acc), 0x134, 0xF, 0xF, true));      // wave_rol:1
+      total = c == 3 && h == 1 ? acc : acc + __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(((lane + 4) & 63) * 4, (int)__float_as_uint(total)));
+    }
+  }
+  return total;
+}
 __device__ __forceinline__ f32x16 zeros16() { return f32x16{}; }
 
 // first kind: tile += rows row0 .. row0 + 31 of LDS x own
@@ -86,7 +110,8 @@ template <typename T, int DH> __device__ __forceinline__ f32x16 rows_product(con
   } else {
 #pragma unroll
     for (int s = 0; s < DH / 8; ++s) {
-      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(row + (((half * (DH / 8) + s) ^ t) << 4));
+      const int low = DH == 32 ? (half * 4 + s) ^ t : (s & 7) ^ t, high = DH == 32 ? 0 : half * (DH / 8) + (s & ~7);
+      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(row + high * 16 + (low << 4));
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], own.f[s][i], acc, 0, 0, 0);
     }
@@ -121,14 +146,14 @@ template <typename T, int DH> __device__ __forceinline__ void columns_product(f3
       }
     }
   } else {
+    const unsigned char* at[4];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int down = 8 * (v >> 2) + 4 * half + (v & 3), t = turn_of<T, DH>(down);
-      const unsigned char* at = lds + (row0 + down) * bytes + (l32 & 3) * 4;
+    for (int i = 0; i < 4; ++i) at[i] = lds + (row0 + 4 * half) * bytes + (((l32 >> 2) ^ (4 * half + i)) << 4) + (l32 & 3) * 4;
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
 #pragma unroll
       for (int f = 0; f < DH / 32; ++f)
-        acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at + (((8 * f + (l32 >> 2)) ^ t) << 4)), tile.w[v], acc[f], 0, 0, 0);
-    }
+        acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at[v & 3] + (8 * (v >> 2) + (v & 3)) * bytes + f * 128), tile.w[v], acc[f], 0, 0, 0);
   }
 }
 
@@ -149,29 +174,28 @@ template <typename T, int DH> __device__ __forceinline__ void columns_exactly(f3
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int c = 32 * f + 8 * (v >> 2) + 4 * half + (v & 3), byte = c * (int)sizeof(T);
-        const float y = as_float(*reinterpret_cast<const T*>(at + ((((byte >> 4) ^ t) << 4) | (byte & 15))));
-        acc[f][v] = on ? __builtin_fmaf(x, y, acc[f][v]) : acc[f][v];
+      for (int v = 0; v < 16; v += 4) {
+        const int byte = (32 * f + 2 * v + 4 * half) * (int)sizeof(T);
+        const T* y = reinterpret_cast<const T*>(at + ((((byte >> 4) ^ t) << 4) | (byte & 15)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[f][v + i] = on ? __builtin_fmaf(x, as_float(y[i]), acc[f][v + i]) : acc[f][v + i];
+        __builtin_amdgcn_sched_barrier(0);                   // few loads at once: this path is rare, its registers count all the same
       }
   }
 }
 
-__device__ __forceinline__ void transfers_done() {      // this wave's global -> LDS transfers have landed
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#endif
-}
-
-// Rows first .. first + ROWS - 1 of a head, straight into LDS; rows past `last` repeat it (whoever reads them hides them).  NW waves share the work.
+// Rows first .. first + ROWS - 1 of a head of two operands, one behind the other, straight into LDS; rows past `last` repeat it (whoever reads them hides them).  NW waves share
+// the pieces of 1 KiB evenly.
 template <typename T, int DH, int ROWS, int NW>
-__device__ __forceinline__ void stage_rows(unsigned char* lds, const T* base, int64_t token, int first, int last, int dim, int wave, int lane) {
-  constexpr int bytes = DH * (int)sizeof(T), per = 1024 / bytes;
-  static_assert(ROWS * bytes % (1024 * NW) == 0, "whole instructions");
+__device__ __forceinline__ void stage_rows(unsigned char* lds, const T* base0, int64_t token0, const T* base1, int64_t token1, int first, int last, int dim, int wave, int lane) {
+  constexpr int bytes = DH * (int)sizeof(T), per = 1024 / bytes, pieces = ROWS * bytes / 1024;
+  static_assert(2 * pieces % NW == 0, "whole instructions");
 #pragma unroll
-  for (int i = 0; i < ROWS * bytes / (1024 * NW); ++i) {
-    const int piece = i * NW + wave, r = piece * per + lane * 16 / bytes, c = (lane & (bytes / 16 - 1)) ^ turn_of<T, DH>(r);
-    const T* src = base + (int64_t)min(first + r, last) * token + c * (16 / (int)sizeof(T));
+  for (int i = 0; i < 2 * pieces / NW; ++i) {
+    const int piece = i * NW + wave;
+    const bool second = piece >= pieces;
+    const int r = (second ? piece - pieces : piece) * per + lane * 16 / bytes, c = (lane & (bytes / 16 - 1)) ^ turn_of<T, DH>(r);
+    const T* src = (second ? base1 : base0) + (int64_t)min(first + r, last) * (second ? token1 : token0) + c * (16 / (int)sizeof(T));
     if (dim != DH) src = c * (16 / (int)sizeof(T)) < dim ? src : reinterpret_cast<const T*>(kZeros);
 #if defined(__HIP_DEVICE_COMPILE__)
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(src), (__attribute__((address_space(3))) void*)(lds + piece * 1024), 16, 0, 0);
@@ -225,69 +249,101 @@ template <typename T, int DH> __device__ __forceinline__ void store_columns(T* r
     }
 }
 
-constexpr int kWaves = 4;                                 // of a block, 32 queries (or keys) each
-constexpr int kBlock = 32 * kWaves;
-template <typename T, int DH> constexpr int stage_rows_of() { return DH * sizeof(T) == 512 ? 32 : 64; }      // keys (or queries) staged at a time
+// A block is NW waves of 32 queries (or keys), which share the rows that they walk.  Those go through a ring of RING stages of ROWS rows of two operands in LDS: the stage in
+// use, the one whose readers may not have finished, and the ones between that are on their way.
+template <typename T, int DH> struct Shape {
+  static constexpr int row = DH * (int)sizeof(T);
+  static constexpr int rows = row >= 256 ? 32 : 64, ring = row >= 512 ? 2 : 4;
+  static constexpr int bytes = rows * row;                  // of one operand's stage
+};
+template <int N> __device__ __forceinline__ void transfers_upto() {      // all but the last N of this wave's transfers have landed
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+#endif
+}
+__device__ __forceinline__ void block_barrier() {      // without __syncthreads' wait for the transfers of later stages
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#endif
+}
+__device__ __forceinline__ int uniform_of(int v) { return __builtin_amdgcn_readfirstlane(v); }
+constexpr int kStatRows = 256;                              // rows of the backward pass's statistics are padded to whole blocks
+__host__ __device__ inline int64_t stat_rows(int n_q) { return ((int64_t)n_q + kStatRows - 1) / kStatRows * kStatRows; }
+
+// Which queries a block works on.  Under the causal mask a block's work grows with its position and a wave's with its queries': blocks go longest first, and with eight waves, of
+// which w and w + 4 share a SIMD, the upper four take their queries in reverse order.
+template <int NW> __device__ __forceinline__ int group_of(int wave, int causal) { return NW == 8 && causal && wave >= 4 ? 11 - wave : wave; }
 
 // ------------------------------------------------------------------------------------------------ forward
-template <typename T, int DH>
-__global__ void __launch_bounds__(64 * kWaves, 2) heads_forward_kernel(AttentionArgs a) {
-  constexpr int KB = stage_rows_of<T, DH>(), BYTES = KB * DH * (int)sizeof(T);
+template <typename T, int DH, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs a) {
+  using Sh = Shape<T, DH>;
+  constexpr int QB = 32 * NW, KB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);      // PER: transfers of a wave for a stage
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int qblocks = (how.n_q + kBlock - 1) / kBlock;
+  const int qblocks = (how.n_q + QB - 1) / QB;
   const int64_t place = place_of_block((int64_t)qblocks * how.n_head * how.batch);
   if (place < 0) return;
   const int64_t bh = place / qblocks;
   const int qb = qblocks - 1 - (int)(place - bh * qblocks), b = (int)(bh / how.n_head), h = (int)(bh - (int64_t)b * how.n_head), hk = h / (how.n_head / how.n_kv_head);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
-  unsigned char* Ks = lds;                                // [2][KB][DH]
-  unsigned char* Vs = lds + 2 * BYTES;
-  float* by_delta = reinterpret_cast<float*>(lds + 4 * BYTES);
+  float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
   const bool biased = how.bias != nullptr;
-  if (biased) stage_bias<T>(by_delta, how, h);
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_q0 = qb * kBlock, q0 = block_q0 + wave * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
-  int kend = min(block_q0 + kBlock, sq.n_q) <= block_q0 ? 0 : sq.n_k;
-  if (causal) kend = min(kend, sq.start + min(block_q0 + kBlock, sq.n_q));
+  const int block_q0 = qb * QB, q0 = block_q0 + group_of<NW>(wave, causal) * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
+  int kend = block_q0 < sq.n_q ? sq.n_k : 0;
+  if (causal) kend = min(kend, sq.start + min(block_q0 + QB, sq.n_q));
   const int stages = kend > 0 ? (kend + KB - 1) / KB : 0;
   int wave_kend = q0 < sq.n_q ? kend : 0;
   if (causal) wave_kend = min(wave_kend, pos0 + 32);
-  Own<T, DH> q;
-  load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, qi < sq.n_q);
   const T* kbase = row_at<T>(a.k, b, 0, hk);
   const T* vbase = row_at<T>(a.v, b, 0, hk);
+  auto stage = [&](int st) {                                // stages past the last are transferred as well (its last row again): every wave then counts the same transfers
+    unsigned char* at = lds + st % Sh::ring * (2 * Sh::bytes);
+    stage_rows<T, DH, KB, NW>(at, kbase, a.k.token, vbase, a.v.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
+  };
   const float scale = how.scale * kLog2e;
+  Own<T, DH> q;
   f32x16 o[DH / 32];
   float mx, lsum;
-  for (int careful = 0;; ++careful) {
+  auto pass = [&](auto again) -> bool {                     // whether a row's result is not finite; again: then once more, with hidden pairs left out of the products (columns_exactly)
+    constexpr bool careful = decltype(again)::value;
+    if (stages)
+#pragma unroll
+      for (int st = 0; st < Sh::ring - 1; ++st) stage(st);
+    if (!careful) {
+      load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, qi < sq.n_q);
+      if (biased) stage_bias<T>(by_delta, how, h);
+    }
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
     mx = -INFINITY, lsum = 0.f;
-    auto stage = [&](int st) {
-      stage_rows<T, DH, KB, kWaves>(Ks + (st & 1) * BYTES, kbase, a.k.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
-      stage_rows<T, DH, KB, kWaves>(Vs + (st & 1) * BYTES, vbase, a.v.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
-    };
-    if (stages) stage(0);
-    transfers_done();
-    __syncthreads();
     for (int st = 0; st < stages; ++st) {
-      if (st + 1 < stages) stage(st + 1);                // into the buffer whose readers are behind the last barrier
-      const unsigned char* K = Ks + (st & 1) * BYTES;
-      const unsigned char* V = Vs + (st & 1) * BYTES;
+      transfers_upto<PER * (Sh::ring - 2)>();
+      block_barrier();
+      stage(st + Sh::ring - 1);                            // where the stage before this one lay, whose readers are behind the barrier
+      const unsigned char* K = lds + st % Sh::ring * (2 * Sh::bytes);
+      const unsigned char* V = K + Sh::bytes;
       for (int kl = 0; kl < KB; kl += 32) {
         const int k0 = st * KB + kl;
         if (k0 >= wave_kend) break;
+        if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, qi < sq.n_q);      // so that it takes no registers beside columns_exactly's
         const f32x16 s = rows_product<T, DH>(K, kl, q, l32, half);
         const bool whole = k0 + 31 < sq.n_k && (!causal || k0 + 31 <= pos0);                     // every query of the wave sees every key of the tile
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;           // the tile has more than one relative position within reach
-        float x[16], top = -INFINITY;
-        uint32_t seen = 0xFFFF;
-        const float flat = biased ? by_delta[k0 < pos0 ? 0 : 2 * reach + 2 * kBiasPad] : 0.f;
-        const float* at = by_delta + (near ? k0 - pos + reach + kBiasPad + 4 * half : 0);
+        float x[16], by = scale, top, flat = 0.f;          // score = by x + flat
+        if (near) {
+          const float* at = by_delta + (k0 - pos + reach + kBiasPad + 4 * half);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, near ? at[8 * (v >> 2) + (v & 3)] : flat);
+          for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, at[8 * (v >> 2) + (v & 3)]);
+          by = 1.0f;
+        } else {
+          if (biased) flat = by_delta[k0 < pos0 ? 0 : 2 * reach + 2 * kBiasPad];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = s[v];
+        }
+        uint32_t seen = 0xFFFF;
         if (!whole) {
           seen = 0;
 #pragma unroll
@@ -298,16 +354,17 @@ __global__ void __launch_bounds__(64 * kWaves, 2) heads_forward_kernel(Attention
             x[v] = on ? x[v] : -INFINITY;
           }
         }
+        top = x[0];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) top = fmaxf(top, x[v]);
-        const float mnew = fmaxf(mx, max_of_halves(top)), msafe = mnew == -INFINITY ? 0.f : mnew;
+        for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+        const float mnew = fmaxf(mx, __builtin_fmaf(max_of_halves(top), by, flat)), msafe = mnew == -INFINITY ? 0.f : mnew, less = flat - msafe;
         const float corr = __builtin_amdgcn_exp2f(mx - msafe);
         float sum = 0.f;
         Tile<T> p;
 #pragma unroll
         for (int v = 0; v < 16; v += 2) {
-          x[v] = __builtin_amdgcn_exp2f(x[v] - msafe);
-          x[v + 1] = __builtin_amdgcn_exp2f(x[v + 1] - msafe);
+          x[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], by, less));
+          x[v + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v + 1], by, less));
           sum += x[v] + x[v + 1];
           put_pair(p, v, x[v], x[v + 1]);
         }
@@ -322,17 +379,17 @@ __global__ void __launch_bounds__(64 * kWaves, 2) heads_forward_kernel(Attention
         if (careful && !whole) columns_exactly<T, DH>(o, V, kl, x, seen, lane);
         else columns_product<T, DH>(o, V, kl, p, lane);
       }
-      transfers_done();
-      __syncthreads();
     }
-    if (careful) break;
+    transfers_upto<0>();                                   // LDS is another's after the last wave
+    if (careful) return false;
     bool bad = false;
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
       for (int v = 0; v < 16; ++v) bad |= !finite(o[f][v]);
-    if (!__syncthreads_or(bad && qi < sq.n_q)) break;
-  }
+    return __syncthreads_or(bad && qi < sq.n_q);
+  };
+  if (pass(std::false_type())) pass(std::true_type());
   if (qi >= how.n_q) return;
   lsum = both_halves(lsum);
   const bool none = qi >= sq.n_q || lsum == 0.f;
@@ -344,84 +401,291 @@ __global__ void __launch_bounds__(64 * kWaves, 2) heads_forward_kernel(Attention
   if (half == 0) a.lse[((int64_t)b * how.n_head + h) * how.n_q + qi] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(lsum)) * kLn2;
 }
 
-// ------------------------------------------------------------------------------------------------ backward: dq, do . o, and the bias gradient's sums by relative position
+// ------------------------------------------------------------------------------------------------ forward, few queries over many keys
+// Bound by the bytes of K and V: the 32 columns of a wave are the queries of all the query heads that share a K/V head, so that those are read once, and every wave walks
+// keys of its own (every kFewWaves-th tile of a chunk), staged for it alone: no barriers, and 2 RING tiles of a block on their way.  Chunks of long sequences are blocks of their own, whose
+// sums heads_join_kernel puts together.
+constexpr int kFewWaves = 2;
+template <typename T, int DH> struct FewShape {
+  static constexpr int row = DH * (int)sizeof(T), tile = 2 * 32 * row, ring = tile <= 8192 ? 4 : 2, per = tile / 1024;
+  static constexpr int join = kFewWaves * (DH * 33 + 64) * 4;      // the waves' results
+  static constexpr int lds = kFewWaves * ring * tile > join ? kFewWaves * ring * tile : join;
+};
+__device__ __forceinline__ void reads_done() {              // this wave's reads of LDS have returned
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#endif
+}
+
+// part: [splits][rows][DH] sums and then [splits][rows][2] maxima (log2) and sums of exponentials, rows = batch n_head n_q; splits == 1: none
 template <typename T, int DH>
-__global__ void __launch_bounds__(64 * kWaves, 2) heads_dq_kernel(AttentionArgs a, float* __restrict__ dots, float* __restrict__ parts) {
-  constexpr int KB = stage_rows_of<T, DH>(), BYTES = KB * DH * (int)sizeof(T);
+__global__ void __launch_bounds__(64 * kFewWaves, DH * sizeof(T) >= 256 ? 1 : 2) heads_few_kernel(AttentionArgs a, int chunk, int splits, float* __restrict__ part) {
+  using Sh = FewShape<T, DH>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int qblocks = (how.n_q + kBlock - 1) / kBlock;
+  const int group = how.n_head / how.n_kv_head, rows = group * how.n_q, row_blocks = (rows + 31) / 32;
+  const int split = (int)(blockIdx.x % (unsigned)splits);
+  const int64_t item = blockIdx.x / (unsigned)splits;
+  const int rb = (int)(item % row_blocks), hk = (int)(item / row_blocks % how.n_kv_head), b = (int)(item / row_blocks / how.n_kv_head);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const Sequence sq = sequence_of(how, b);
+  const int r = rb * 32 + l32, head = min(r, rows - 1) / how.n_q, i = min(r, rows - 1) - head * how.n_q, h = hk * group + head;
+  const bool valid = r < rows && i < sq.n_q;
+  // positions of the block's queries: of one head, or all
+  const int first_row = rb * 32, last_row = min(rows, first_row + 32) - 1;
+  const bool one_head = first_row / how.n_q == last_row / how.n_q;
+  const int i_low = one_head ? first_row % how.n_q : 0, i_high = min(one_head ? last_row % how.n_q : how.n_q - 1, sq.n_q - 1);
+  const int pos = sq.start + i, pos_low = sq.start + i_low, pos_high = sq.start + i_high;
+  const int causal = how.causal, reach = how.bias_reach;
+  const bool biased = how.bias != nullptr;
+  int kend = i_low <= i_high ? sq.n_k : 0;
+  if (causal) kend = min(kend, pos_high + 1);
+  const int kbegin = split * chunk;
+  kend = min(kend, kbegin + chunk);
+  const int tiles = kend > kbegin ? (kend - kbegin + 31) / 32 : 0, mine = tiles > wave ? (tiles - wave + kFewWaves - 1) / kFewWaves : 0;
+  const T* kbase = row_at<T>(a.k, b, 0, hk);
+  const T* vbase = row_at<T>(a.v, b, 0, hk);
+  unsigned char* ring = lds + wave * Sh::ring * Sh::tile;
+  auto stage = [&](int n) {                                 // this wave's n-th tile; past the last one its last row again
+    stage_rows<T, DH, 32, 1>(ring + n % Sh::ring * Sh::tile, kbase, a.k.token, vbase, a.v.token, min(kbegin + (n * kFewWaves + wave) * 32, sq.n_k - 1), sq.n_k - 1, how.head_dim, 0, lane);
+  };
+  const float scale = how.scale * kLog2e;
+  auto bias_at = [&](int delta) {                           // a column's own head: looked up where the tables lie
+    const int bucket = how.bias_map[min(max(delta, -reach), reach) + reach];
+    return bucket >= 0 && bucket < how.bias_buckets ? as_float(((const T*)how.bias)[(int64_t)bucket * how.n_head + h]) * kLog2e : __uint_as_float(0x7FC00000u);
+  };
+  Own<T, DH> q;
+  f32x16 o[DH / 32];
+  float mx, lsum, flat_low = 0.f, flat_high = 0.f;
+  auto pass = [&](auto again) -> bool {
+    constexpr bool careful = decltype(again)::value;
+    if (mine)
+#pragma unroll
+      for (int n = 0; n < Sh::ring - 1; ++n) stage(n);
+    if (!careful) {
+      load_own<T, DH>(q, row_at<T>(a.q, b, i, h), half, how.head_dim, valid);
+      if (biased) { flat_low = bias_at(-reach); flat_high = bias_at(reach); }
+    }
+#pragma unroll
+    for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
+    mx = -INFINITY, lsum = 0.f;
+    for (int n = 0; n < mine; ++n) {
+      reads_done();                                         // of the tile whose place the next transfers take
+      stage(n + Sh::ring - 1);
+      transfers_upto<Sh::per * (Sh::ring - 1)>();
+      const unsigned char* K = ring + n % Sh::ring * Sh::tile;
+      const unsigned char* V = K + Sh::tile / 2;
+      const int k0 = kbegin + (n * kFewWaves + wave) * 32;
+      if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, i, h), half, how.head_dim, valid);
+      const f32x16 s = rows_product<T, DH>(K, 0, q, l32, half);
+      const bool whole = k0 + 31 < sq.n_k && (!causal || k0 + 31 <= pos_low);
+      const bool near = biased && k0 + 31 - pos_low > -reach && k0 - pos_high < reach;
+      float x[16];
+      const float flat = k0 < pos_low ? flat_low : flat_high;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, flat);
+      if (near) {
+        float by[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) by[v] = bias_at(k0 + 8 * (v >> 2) + 4 * half + (v & 3) - pos);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, by[v]);
+      }
+      uint32_t seen = 0xFFFF;
+      if (!whole) {
+        seen = 0;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int key = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
+          const bool on = key < sq.n_k && (!causal || key <= pos);
+          seen |= (uint32_t)on << v;
+          x[v] = on ? x[v] : -INFINITY;
+        }
+      }
+      float top = x[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+      const float mnew = fmaxf(mx, max_of_halves(top)), msafe = mnew == -INFINITY ? 0.f : mnew;
+      const float corr = __builtin_amdgcn_exp2f(mx - msafe);
+      float sum = 0.f;
+      Tile<T> p;
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) {
+        x[v] = __builtin_amdgcn_exp2f(x[v] - msafe);
+        x[v + 1] = __builtin_amdgcn_exp2f(x[v + 1] - msafe);
+        sum += x[v] + x[v + 1];
+        put_pair(p, v, x[v], x[v + 1]);
+      }
+      lsum = __builtin_fmaf(lsum, corr, sum);
+      mx = mnew;
+#pragma unroll
+      for (int f = 0; f < DH / 32; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[f][v] *= corr;
+      if (careful && !whole) columns_exactly<T, DH>(o, V, 0, x, seen, lane);
+      else columns_product<T, DH>(o, V, 0, p, lane);
+    }
+    transfers_upto<0>();
+    if (careful) return false;
+    bool bad = false;
+#pragma unroll
+    for (int f = 0; f < DH / 32; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) bad |= !finite(o[f][v]);
+    return __builtin_amdgcn_ballot_w64(bad && valid) != 0;
+  };
+  if (pass(std::false_type())) pass(std::true_type());
+  lsum = both_halves(lsum);
+  __syncthreads();
+  float* joined = reinterpret_cast<float*>(lds);            // [waves][DH][33], then [waves][32][2]
+  float* stats = joined + kFewWaves * DH * 33;
+#pragma unroll
+  for (int f = 0; f < DH / 32; ++f)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) joined[(wave * DH + 32 * f + 8 * (v >> 2) + 4 * half + (v & 3)) * 33 + l32] = o[f][v];
+  if (half == 0) { stats[(wave * 32 + l32) * 2] = mx; stats[(wave * 32 + l32) * 2 + 1] = lsum; }
+  __syncthreads();
+  const int64_t all_rows = (int64_t)how.batch * how.n_head * how.n_q;
+  for (int at = tid; at < min(32, rows - first_row) * DH; at += 64 * kFewWaves) {
+    const int rr = at / DH, c = at % DH, hh = hk * group + (first_row + rr) / how.n_q, ii = (first_row + rr) % how.n_q;
+    const float m0 = stats[rr * 2], m1 = stats[(32 + rr) * 2], m = fmaxf(m0, m1), safe = m == -INFINITY ? 0.f : m;
+    const float w0 = __builtin_amdgcn_exp2f(m0 - safe), w1 = __builtin_amdgcn_exp2f(m1 - safe);
+    const float v = joined[c * 33 + rr] * w0 + joined[(DH + c) * 33 + rr] * w1, l = stats[rr * 2 + 1] * w0 + stats[(32 + rr) * 2 + 1] * w1;
+    const int64_t row = ((int64_t)b * how.n_head + hh) * how.n_q + ii;
+    if (splits == 1) {
+      const bool none = ii >= sq.n_q || l == 0.f;
+      if (c < how.head_dim) put_float(none ? 0.f : v / l, const_cast<T*>(row_at<T>(a.out, b, ii, hh)) + c);
+      if (c == 0) a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    } else {
+      if (m != -INFINITY) part[((int64_t)split * all_rows + row) * DH + c] = v;      // not read otherwise
+      if (c == 0) {
+        float* st = part + (int64_t)splits * all_rows * DH + ((int64_t)split * all_rows + row) * 2;
+        st[0] = ii >= sq.n_q ? -INFINITY : m;
+        st[1] = l;
+      }
+    }
+  }
+}
+
+// The chunks' sums of a row: a wave each.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, int splits, const float* __restrict__ part) {
+  const zgr_attention& how = a.how;
+  const int64_t all_rows = (int64_t)how.batch * how.n_head * how.n_q, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= all_rows) return;
+  const int lane = threadIdx.x & 63;
+  const float* stats = part + (int64_t)splits * all_rows * DH;
+  float m = -INFINITY;
+  for (int s = lane; s < splits; s += 64) m = fmaxf(m, stats[((int64_t)s * all_rows + row) * 2]);
+  m = wave_max(m);
+  const int b = (int)(row / ((int64_t)how.n_head * how.n_q)), h = (int)(row / how.n_q % how.n_head), i = (int)(row % how.n_q);
+  constexpr int PER = DH / 64 > 0 ? DH / 64 : 1;
+  float o[PER] = {}, l = 0.f;
+  if (m != -INFINITY) {
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const int64_t at = (int64_t)s * all_rows + row;
+      const float ms = stats[at * 2], w = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - m);      // a chunk without a visible key left nothing to weigh
+      l += w * stats[at * 2 + 1];
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int c = lane * PER + j;
+        if (c < DH && w != 0.f) o[j] += w * part[at * DH + c];
+      }
+    }
+  }
+  const bool none = l == 0.f;
+  T* out = const_cast<T*>(row_at<T>(a.out, b, i, h));
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (lane * PER + j < how.head_dim) put_float(none ? 0.f : o[j] / l, out + lane * PER + j);
+  if (lane == 0) a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------------------------ backward: dq, the rows' statistics, and the bias gradient's sums by relative position
+// stats: [batch][head][2][stat_rows]: log2 of each row's sum of exponentials, +infinity for a row that has no probabilities, and do . o.
+template <typename T, int DH, int NW>
+__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_dq_kernel(AttentionArgs a, float* __restrict__ stats, float* __restrict__ parts) {
+  using Sh = Shape<T, DH>;
+  constexpr int QB = 32 * NW, KB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  const zgr_attention& how = a.how;
+  const int qblocks = (how.n_q + QB - 1) / QB;
   const int64_t place = place_of_block((int64_t)qblocks * how.n_head * how.batch);
   if (place < 0) return;
   const int64_t bh = place / qblocks;
   const int qb = qblocks - 1 - (int)(place - bh * qblocks), b = (int)(bh / how.n_head), h = (int)(bh - (int64_t)b * how.n_head), hk = h / (how.n_head / how.n_kv_head);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
-  unsigned char* Ks = lds;
-  unsigned char* Vs = lds + 2 * BYTES;
-  float* by_delta = reinterpret_cast<float*>(lds + 4 * BYTES);
+  float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
   const bool biased = how.bias != nullptr;
   const int places = bias_places(how);
-  float* bins = reinterpret_cast<float*>(lds + 4 * BYTES + bias_bytes(how)) + (2 * wave + half) * places;      // sums by relative position, for each half of each wave
-  if (biased) stage_bias<T>(by_delta, how, h);
+  float* all_bins = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes + bias_bytes(how));
+  float* bins = all_bins + wave * places;                   // each wave's sums by relative position
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_q0 = qb * kBlock, q0 = block_q0 + wave * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
-  int kend = min(block_q0 + kBlock, sq.n_q) <= block_q0 ? 0 : sq.n_k;
-  if (causal) kend = min(kend, sq.start + min(block_q0 + kBlock, sq.n_q));
+  const int block_q0 = qb * QB, q0 = block_q0 + group_of<NW>(wave, causal) * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
+  int kend = block_q0 < sq.n_q ? sq.n_k : 0;
+  if (causal) kend = min(kend, sq.start + min(block_q0 + QB, sq.n_q));
   const int stages = kend > 0 ? (kend + KB - 1) / KB : 0;
   int wave_kend = q0 < sq.n_q ? kend : 0;
   if (causal) wave_kend = min(wave_kend, pos0 + 32);
   const bool valid = qi < sq.n_q;
-  Own<T, DH> q, d;
-  load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, valid);
-  load_own<T, DH>(d, row_at<T>(a.dout, b, qi, h), half, how.head_dim, valid);
-  float dot;
-  {
-    Own<T, DH> o;
-    load_own<T, DH>(o, row_at<T>(a.out, b, qi, h), half, how.head_dim, valid);
-    dot = both_halves(dot_own<T, DH>(o, d));
-  }
-  const int64_t stat = ((int64_t)b * how.n_head + h) * how.n_q + qi;
-  // p = exp2(x - lse): a row that is none of the sequence's, or sees nothing, gets zeros
-  const float lse_log2 = valid ? a.lse[stat] * kLog2e : INFINITY, lse = lse_log2 == -INFINITY ? INFINITY : lse_log2;
-  if (valid && half == 0) dots[stat] = dot;
   const T* kbase = row_at<T>(a.k, b, 0, hk);
   const T* vbase = row_at<T>(a.v, b, 0, hk);
+  auto stage = [&](int st) {
+    unsigned char* at = lds + st % Sh::ring * (2 * Sh::bytes);
+    stage_rows<T, DH, KB, NW>(at, kbase, a.k.token, vbase, a.v.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
+  };
   const float scale = how.scale * kLog2e;
+  Own<T, DH> q, d;
+  float dot = 0.f, lse = INFINITY;
   f32x16 dq[DH / 32];
   float below = 0.f, above = 0.f;                         // sums beyond reach
-  for (int careful = 0;; ++careful) {
+  auto pass = [&](auto again) -> bool {                     // whether a row's result is not finite; again: then once more, with hidden pairs left out of the products (columns_exactly)
+    constexpr bool careful = decltype(again)::value;
+    if (stages)
+#pragma unroll
+      for (int st = 0; st < Sh::ring - 1; ++st) stage(st);
+    if (!careful) {
+      load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, valid);
+      load_own<T, DH>(d, row_at<T>(a.dout, b, qi, h), half, how.head_dim, valid);
+      if (valid) lse = a.lse[((int64_t)b * how.n_head + h) * how.n_q + qi] * kLog2e;
+      if (lse == -INFINITY) lse = INFINITY;               // p = exp2(x - lse)
+      Own<T, DH> o;
+      load_own<T, DH>(o, row_at<T>(a.out, b, qi, h), half, how.head_dim, valid);
+      dot = both_halves(dot_own<T, DH>(o, d));
+      if (biased) stage_bias<T>(by_delta, how, h);
+    }
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) dq[f] = zeros16();
     below = above = 0.f;
-    if (biased) for (int i = l32; i < places; i += 32) bins[i] = 0.f;
-    auto stage = [&](int st) {
-      stage_rows<T, DH, KB, kWaves>(Ks + (st & 1) * BYTES, kbase, a.k.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
-      stage_rows<T, DH, KB, kWaves>(Vs + (st & 1) * BYTES, vbase, a.v.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
-    };
-    if (stages) stage(0);
-    transfers_done();
-    __syncthreads();
+    if (biased) for (int i = lane; i < places; i += 64) bins[i] = 0.f;
     for (int st = 0; st < stages; ++st) {
-      if (st + 1 < stages) stage(st + 1);
-      const unsigned char* K = Ks + (st & 1) * BYTES;
-      const unsigned char* V = Vs + (st & 1) * BYTES;
+      transfers_upto<PER * (Sh::ring - 2)>();
+      block_barrier();
+      stage(st + Sh::ring - 1);
+      const unsigned char* K = lds + st % Sh::ring * (2 * Sh::bytes);
+      const unsigned char* V = K + Sh::bytes;
       for (int kl = 0; kl < KB; kl += 32) {
         const int k0 = st * KB + kl;
         if (k0 >= wave_kend) break;
+        if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, valid);
         const f32x16 s = rows_product<T, DH>(K, kl, q, l32, half);
+        if (careful) load_own<T, DH>(d, row_at<T>(a.dout, b, qi, h), half, how.head_dim, valid);
         const f32x16 dp = rows_product<T, DH>(V, kl, d, l32, half);
         const bool whole = k0 + 31 < sq.n_k && q0 + 31 < sq.n_q && (!causal || k0 + 31 <= pos0);
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;
-        const float flat = biased ? by_delta[k0 < pos0 ? 0 : 2 * reach + 2 * kBiasPad] : 0.f;
         const int first = near ? k0 - pos + reach + kBiasPad + 4 * half : 0;
-        float ds[16];
-        uint32_t seen = 0xFFFF;
+        float ds[16];                                     // p, and then its gradient
+        if (near) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float x = __builtin_fmaf(s[v], scale, near ? by_delta[first + 8 * (v >> 2) + (v & 3)] : flat);
-          ds[v] = __builtin_amdgcn_exp2f(x - lse) * (dp[v] - dot);
+          for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, by_delta[first + 8 * (v >> 2) + (v & 3)]) - lse);
+        } else {
+          const float less = (biased ? by_delta[k0 < pos0 ? 0 : 2 * reach + 2 * kBiasPad] : 0.f) - lse;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, less));
         }
+        uint32_t seen = 0xFFFF;
         if (!whole) {
           seen = 0;
 #pragma unroll
@@ -429,55 +693,82 @@ __global__ void __launch_bounds__(64 * kWaves, 2) heads_dq_kernel(AttentionArgs 
             const int key = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
             const bool on = valid && key < sq.n_k && (!causal || key <= pos);
             seen |= (uint32_t)on << v;
-            ds[v] = on ? ds[v] : 0.f;
           }
+        }
+        if (wave_kend <= 32) {
+          // All of the rows' probabilities are here: do . o as the sum of p dp, which is what it stands for.  In rows that see few keys the rounding of `out` would be
+          // a good part of dp - do . o (16 x 256 causal rows of bf16: dq off by 0.0026 of its norm, of which its own rounding is 0.0017).
+          float sum = 0.f;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) sum += (seen >> v) & 1 ? ds[v] * dp[v] : 0.f;
+          dot = both_halves(sum);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) ds[v] *= dp[v] - dot;
+        if (!whole) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) ds[v] = (seen >> v) & 1 ? ds[v] : 0.f;
         }
         Tile<T> t;
 #pragma unroll
         for (int v = 0; v < 16; v += 2) put_pair(t, v, ds[v], ds[v + 1]);
-        if (biased) {
-          // The lanes of a half hold 32 different relative positions of one key, and each half of each wave has sums of its own: no two lanes add to one
-          // place at once, so the order of the sums is the program's.
-          if (near) {
+        if (near) {
+          float* bin = bins + (k0 - pos0 + reach + kBiasPad - (half ? lane - 64 : lane));
+          const float sum = diagonal_sums(ds, lane);
+          if (lane != 32) *bin += sum;                      // t = -32 is no diagonal
+        } else if (biased) {
+          float sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) __hip_atomic_fetch_add(bins + first + 8 * (v >> 2) + (v & 3), ds[v], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-          } else {
-            float sum = 0.f;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) sum += ds[v];
-            below += k0 < pos0 ? sum : 0.f;
-            above += k0 < pos0 ? 0.f : sum;
-          }
+          for (int v = 0; v < 16; ++v) sum += ds[v];
+          if (k0 < pos0) below += sum;
+          else above += sum;
         }
         if (careful && !whole) columns_exactly<T, DH>(dq, K, kl, ds, seen, lane);
         else columns_product<T, DH>(dq, K, kl, t, lane);
       }
-      transfers_done();
-      __syncthreads();
     }
-    if (careful) break;
+    transfers_upto<0>();
+    if (careful) return false;
     bool bad = false;
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
       for (int v = 0; v < 16; ++v) bad |= !finite(dq[f][v]);
-    if (!__syncthreads_or(bad && valid)) break;
+    return __syncthreads_or(bad && valid);
+  };
+  if (pass(std::false_type())) pass(std::true_type());
+  if (half == 0) {
+    float* stat = stats + ((int64_t)b * how.n_head + h) * 2 * stat_rows(how.n_q) + qi;
+    stat[0] = lse;
+    stat[stat_rows(how.n_q)] = dot;
   }
   if (biased && parts) {
-    float* ends = reinterpret_cast<float*>(lds);          // the operands are behind the last barrier
-    ends[tid] = below;
-    ends[64 * kWaves + tid] = above;
+    float* ends = reinterpret_cast<float*>(lds);            // the operands have been read
+    below = wave_sum(below), above = wave_sum(above);
+    __syncthreads();
+    if (lane == 0) ends[wave] = below, ends[NW + wave] = above;
+    for (int j = tid; j < places; j += 64 * NW) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) v += all_bins[w * places + j];
+      all_bins[j] = v;
+    }
     __syncthreads();
     float* part = parts + (((int64_t)h * how.batch + b) * qblocks + qb) * (2 * reach + 1);
-    const float* all = reinterpret_cast<const float*>(lds + 4 * BYTES + bias_bytes(how));
-    for (int i = tid; i <= 2 * reach; i += 64 * kWaves) {
-      float v = 0.f;
-      const int lo = i == 0 ? 0 : i + kBiasPad, hi = i == 2 * reach ? places - 1 : i + kBiasPad;
-      for (int j = lo; j <= hi; ++j)
-        for (int w = 0; w < 2 * kWaves; ++w) v += all[w * places + j];
-      if (i == 0) for (int j = 0; j < 64 * kWaves; ++j) v += ends[j];
-      if (i == 2 * reach) for (int j = 0; j < 64 * kWaves; ++j) v += ends[64 * kWaves + j];
-      part[i] = v;
+    for (int i = 1 + tid; i < 2 * reach; i += 64 * NW) part[i] = all_bins[i + kBiasPad];
+    if (wave < 2) {                                         // wave 0: what lies at -reach and below, wave 1: at reach and above
+      const int last = places - 1 - lane;
+      float v = wave == 0 ? all_bins[lane] : all_bins[last];
+      static_assert(kBiasPad == 64, "a place for each lane, and one more");
+      if (lane == 0 && (wave == 0 || reach > 0)) v += wave == 0 ? all_bins[kBiasPad] : all_bins[kBiasPad + 2 * reach];
+      if (lane < NW) v += ends[NW * wave + lane];
+      v = wave_sum(v);
+      if (reach > 0) { if (lane == 0) part[wave * 2 * reach] = v; }
+      else if (lane == 0) ends[2 * NW + wave] = v;
+    }
+    if (reach == 0) {
+      __syncthreads();
+      if (tid == 0) part[0] = ends[2 * NW] + ends[2 * NW + 1];
     }
   }
   if (qi >= how.n_q) return;
@@ -488,25 +779,24 @@ __global__ void __launch_bounds__(64 * kWaves, 2) heads_dq_kernel(AttentionArgs 
 }
 
 // ------------------------------------------------------------------------------------------------ backward: dk, dv
-template <typename T, int DH>
-__global__ void __launch_bounds__(64 * kWaves, DH == 128 ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ dots) {
-  constexpr int QB = stage_rows_of<T, DH>(), BYTES = QB * DH * (int)sizeof(T);
+template <typename T, int DH, int NW>
+__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ stats) {
+  using Sh = Shape<T, DH>;
+  constexpr int KB = 32 * NW, QB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int kblocks = (how.n_k + kBlock - 1) / kBlock, group = how.n_head / how.n_kv_head;
+  const int kblocks = (how.n_k + KB - 1) / KB, group = how.n_head / how.n_kv_head;
   const int64_t place = place_of_block((int64_t)kblocks * how.n_kv_head * how.batch);
   if (place < 0) return;
   const int64_t bh = place / kblocks;
   const int kb = (int)(place - bh * kblocks), b = (int)(bh / how.n_kv_head), hk = (int)(bh - (int64_t)b * how.n_kv_head);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
-  unsigned char* Qs = lds;
-  unsigned char* Ds = lds + 2 * BYTES;
-  float* stats = reinterpret_cast<float*>(lds + 4 * BYTES);      // [2][2][QB]: lse in log2 units, do . o
-  float* by_delta = stats + 4 * QB;
+  float* rows_stats = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);      // [ring][2][64]
+  float* by_delta = rows_stats + Sh::ring * 128;
   const bool biased = how.bias != nullptr;
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_k0 = kb * kBlock, k0 = block_k0 + wave * 32, kj = k0 + l32;
+  const int block_k0 = kb * KB, k0 = block_k0 + group_of<NW>(wave, causal) * 32, kj = k0 + l32;
   const bool valid = kj < sq.n_k;
   // the first query that sees a key of the block, and of the wave
   int qbegin = causal ? max(0, block_k0 - sq.start) : 0, wave_qbegin = causal ? max(0, k0 - sq.start) : 0;
@@ -514,57 +804,78 @@ __global__ void __launch_bounds__(64 * kWaves, DH == 128 ? 1 : 2) heads_dkv_kern
   if (k0 >= sq.n_k) wave_qbegin = sq.n_q;
   qbegin = qbegin / QB * QB;
   const int per_head = sq.n_q > qbegin ? (sq.n_q - qbegin + QB - 1) / QB : 0, stages = per_head * group;
-  Own<T, DH> k, vv;
-  load_own<T, DH>(k, row_at<T>(a.k, b, kj, hk), half, how.head_dim, valid);
-  load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
+  const int64_t n_stats = stat_rows(how.n_q);
+  struct At { int st, h, first; };                          // a stage's number, head and first query
+  auto stage = [&](const At& at) {
+    unsigned char* to = lds + at.st % Sh::ring * (2 * Sh::bytes);
+    stage_rows<T, DH, QB, NW>(to, row_at<T>(a.q, b, 0, at.h), a.q.token, row_at<T>(a.dout, b, 0, at.h), a.dout.token, at.first, sq.n_q - 1, how.head_dim, wave, lane);
+    if (wave < 2) {                                         // the rows' statistics (64 of them, of which a stage of 32 rows uses half)
+      const float* src = stats + ((int64_t)b * how.n_head + at.h) * 2 * n_stats + wave * n_stats + min((int64_t)at.first + lane, n_stats - 1);
+#if defined(__HIP_DEVICE_COMPILE__)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(src), (__attribute__((address_space(3))) void*)(rows_stats + at.st % Sh::ring * 128 + wave * 64), 4, 0, 0);
+#endif
+    }
+  };
+  auto next = [&](At& at) {                                 // past the last stage its rows again: every wave counts the same transfers
+    ++at.st;
+    if (at.first + QB < sq.n_q) at.first += QB;
+    else if (at.h + 1 < (hk + 1) * group) { ++at.h; at.first = qbegin; }
+  };
   const float scale = how.scale * kLog2e;
+  Own<T, DH> k, vv;
   f32x16 dk[DH / 32], dv[DH / 32];
-  for (int careful = 0;; ++careful) {
+  auto pass = [&](auto again) -> bool {                     // whether a row's result is not finite; again: then once more, with hidden pairs left out of the products (columns_exactly)
+    constexpr bool careful = decltype(again)::value;
+    At ahead{0, hk * group, qbegin};
+    if (stages)
+#pragma unroll
+      for (int i = 0; i < Sh::ring - 1; ++i) { stage(ahead); next(ahead); }
+    if (!careful) {
+      load_own<T, DH>(k, row_at<T>(a.k, b, kj, hk), half, how.head_dim, valid);
+      load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
+    }
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) dk[f] = dv[f] = zeros16();
-    auto stage = [&](int st) {
-      const int h = hk * group + st / per_head, first = qbegin + st % per_head * QB, buf = st & 1;
-      stage_rows<T, DH, QB, kWaves>(Qs + buf * BYTES, row_at<T>(a.q, b, 0, h), a.q.token, first, sq.n_q - 1, how.head_dim, wave, lane);
-      stage_rows<T, DH, QB, kWaves>(Ds + buf * BYTES, row_at<T>(a.dout, b, 0, h), a.dout.token, first, sq.n_q - 1, how.head_dim, wave, lane);
-      if (tid < QB) {
-        const int64_t stat = ((int64_t)b * how.n_head + h) * how.n_q + first + tid;
-        const float lse = first + tid < sq.n_q ? a.lse[stat] * kLog2e : INFINITY;
-        stats[buf * 2 * QB + tid] = lse == -INFINITY ? INFINITY : lse;
-        stats[buf * 2 * QB + QB + tid] = first + tid < sq.n_q ? dots[stat] : 0.f;
+    At here{0, hk * group, qbegin};
+    for (int st = 0; st < stages; ++st, next(here)) {
+      if (here.first == qbegin && biased) {                 // another head
+        if (st) block_barrier();
+        stage_bias<T>(by_delta, how, here.h);
       }
-    };
-    if (stages) stage(0);
-    for (int st = 0; st < stages; ++st) {
-      const int h = hk * group + st / per_head;
-      if (st % per_head == 0 && biased) {                 // another head
-        if (st) __syncthreads();
-        stage_bias<T>(by_delta, how, h);
-      }
-      transfers_done();
-      __syncthreads();
-      if (st + 1 < stages) stage(st + 1);
-      const unsigned char* Q = Qs + (st & 1) * BYTES;
-      const unsigned char* D = Ds + (st & 1) * BYTES;
-      const float* lses = stats + (st & 1) * 2 * QB + 4 * half;
+      if (wave < 2) transfers_upto<(PER + 1) * (Sh::ring - 2)>();
+      else transfers_upto<PER * (Sh::ring - 2)>();
+      block_barrier();
+      stage(ahead);
+      next(ahead);
+      const unsigned char* Q = lds + st % Sh::ring * (2 * Sh::bytes);
+      const unsigned char* D = Q + Sh::bytes;
+      const float* lses = rows_stats + st % Sh::ring * 128 + 4 * half;
       for (int ql = 0; ql < QB; ql += 32) {
-        const int q0 = qbegin + st % per_head * QB + ql, pos0 = sq.start + q0;
+        const int q0 = here.first + ql, pos0 = sq.start + q0;
         if (q0 >= sq.n_q) break;
         if (q0 + 31 < wave_qbegin) continue;
+        if (careful) load_own<T, DH>(k, row_at<T>(a.k, b, kj, hk), half, how.head_dim, valid);
         const f32x16 s = rows_product<T, DH>(Q, ql, k, l32, half);
+        if (careful) load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
         const f32x16 dp = rows_product<T, DH>(D, ql, vv, l32, half);
         const bool whole = k0 + 31 < sq.n_k && q0 + 31 < sq.n_q && (!causal || k0 + 31 <= pos0);
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;
-        const float flat = biased ? by_delta[k0 < pos0 ? 0 : 2 * reach + 2 * kBiasPad] : 0.f;
-        const int first = near ? kj - pos0 + reach + kBiasPad - 4 * half : 31;
         float p[16], ds[16];
-        uint32_t seen = 0xFFFF;
+        if (near) {
+          const float* at = by_delta + (kj - pos0 + reach + kBiasPad - 4 * half);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int r = 8 * (v >> 2) + (v & 3);
-          const float x = __builtin_fmaf(s[v], scale, near ? by_delta[first - r] : flat);
-          p[v] = __builtin_amdgcn_exp2f(x - lses[ql + r]);
-          ds[v] = p[v] * (dp[v] - lses[QB + ql + r]);
+          for (int v = 0; v < 16; ++v) {
+            const int r = 8 * (v >> 2) + (v & 3);
+            p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, at[-r]) - lses[ql + r]);
+          }
+        } else {
+          const float flat = biased ? by_delta[k0 < pos0 ? 0 : 2 * reach + 2 * kBiasPad] : 0.f;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, flat - lses[ql + 8 * (v >> 2) + (v & 3)]));
         }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) ds[v] = p[v] * (dp[v] - lses[64 + ql + 8 * (v >> 2) + (v & 3)]);
+        uint32_t seen = 0xFFFF;
         if (!whole) {
           seen = 0;
 #pragma unroll
@@ -591,14 +902,16 @@ __global__ void __launch_bounds__(64 * kWaves, DH == 128 ? 1 : 2) heads_dkv_kern
         }
       }
     }
-    if (careful) break;
+    transfers_upto<0>();
+    if (careful) return false;
     bool bad = false;
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
       for (int v = 0; v < 16; ++v) bad |= !finite(dk[f][v]) || !finite(dv[f][v]);
-    if (!__syncthreads_or(bad && valid)) break;
-  }
+    return __syncthreads_or(bad && valid);
+  };
+  if (pass(std::false_type())) pass(std::true_type());
   if (kj >= how.n_k) return;
   if (!valid)
 #pragma unroll
@@ -614,6 +927,7 @@ __global__ void __launch_bounds__(1024) heads_dbias_kernel(zgr_attention how, co
   const int h = blockIdx.x, n = 2 * how.bias_reach + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int i = threadIdx.x; i < n; i += 1024) {
     float v = 0.f;
+#pragma unroll 8
     for (int p = 0; p < n_parts; ++p) v += parts[((int64_t)h * n_parts + p) * n + i];
     sums[i] = v;
   }
@@ -627,40 +941,67 @@ __global__ void __launch_bounds__(1024) heads_dbias_kernel(zgr_attention how, co
   }
 }
 
-template <typename T, int DH> int forward_lds(const zgr_attention& how) { return 4 * stage_rows_of<T, DH>() * DH * (int)sizeof(T) + bias_bytes(how); }
-template <typename T, int DH> int dq_lds(const zgr_attention& how) { return forward_lds<T, DH>(how) + bias_places(how) * 4 * 2 * kWaves; }
-template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return forward_lds<T, DH>(how) + 4 * stage_rows_of<T, DH>() * 4; }
+template <typename T, int DH> int ring_bytes() { return Shape<T, DH>::ring * 2 * Shape<T, DH>::bytes; }
+template <typename T, int DH> int forward_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + bias_bytes(how); }
+template <typename T, int DH, int NW> int dq_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + bias_bytes(how) + bias_places(how) * 4 * NW; }
+template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + Shape<T, DH>::ring * 128 * 4 + bias_bytes(how); }
 
-unsigned blocks_for(int64_t work) { return (unsigned)((work + 7) / 8 * 8); }      // place_of_block deals them out in eights
-
-template <typename K> hipError_t with_lds(K kernel, int bytes) {
-  return bytes > 65536 ? hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
-}
-
-template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStream_t s) {
-  const int64_t blocks = (int64_t)((a.how.n_q + kBlock - 1) / kBlock) * a.how.n_head * a.how.batch;
-  const int lds = forward_lds<T, DH>(a.how);
-  if (hipError_t e = with_lds(heads_forward_kernel<T, DH>, lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL((heads_forward_kernel<T, DH>), dim3(blocks_for(blocks)), dim3(64 * kWaves), lds, s, a);
+template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), int64_t blocks, int threads, int lds, hipStream_t s, A... args) {
+  if (!blocks) return hipSuccess;
+  if (lds > 65536)
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, s, args...);
   return hipGetLastError();
 }
 
-size_t dots_bytes(const zgr_attention& how) { return ((size_t)how.batch * how.n_head * how.n_q * 4 + 255) / 256 * 256; }
-int parts_of(const zgr_attention& how) { return how.batch * ((how.n_q + kBlock - 1) / kBlock); }
+constexpr int kForwardWaves = 4, kQueryWaves = 4, kKeyWaves = 4;
+int64_t blocks_of(int n, int block, int heads, int batch) { return (int64_t)((n + block - 1) / block) * heads * batch; }
+
+// Few queries: those of the heads that share a K/V head fit two waves' columns, or the blocks of the other kernel would leave most of the chip idle over many keys.
+bool few_queries(const zgr_attention& how) {
+  const int64_t rows = (int64_t)(how.n_head / how.n_kv_head) * how.n_q;
+  return rows <= 64 || (blocks_of(how.n_q, 32 * kForwardWaves, how.n_head, how.batch) <= 128 && how.n_k >= 1024);
+}
+// Chunks: some 2048 blocks in all, of 64 keys at least (a tile for each wave).
+struct Chunks { int keys, splits; int64_t blocks; };
+Chunks chunks_of(const zgr_attention& how) {
+  const int64_t items = ((int64_t)(how.n_head / how.n_kv_head) * how.n_q + 31) / 32 * how.n_kv_head * how.batch;
+  int64_t keys = ((int64_t)how.n_k * items + 2047) / 2048;
+  keys = (keys + 63) / 64 * 64;
+  if (keys < 64) keys = 64;
+  Chunks c;
+  c.keys = (int)keys;
+  c.splits = how.n_k ? (int)((how.n_k + keys - 1) / keys) : 1;
+  c.blocks = items * c.splits;
+  return c;
+}
+size_t part_bytes(const zgr_attention& how, int dh) {
+  if (!few_queries(how)) return 0;
+  const Chunks c = chunks_of(how);
+  return c.splits == 1 ? 0 : ((size_t)c.splits * how.batch * how.n_head * how.n_q * (dh + 2) * 4 + 255) / 256 * 256;
+}
+
+template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStream_t s) {
+  if (!few_queries(a.how))
+    return start(heads_forward_kernel<T, DH, kForwardWaves>, (blocks_of(a.how.n_q, 32 * kForwardWaves, a.how.n_head, a.how.batch) + 7) / 8 * 8, 64 * kForwardWaves, forward_lds<T, DH>(a.how), s, a);
+  const Chunks c = chunks_of(a.how);
+  float* part = reinterpret_cast<float*>(a.workspace);
+  hipError_t e = start(heads_few_kernel<T, DH>, c.blocks, 64 * kFewWaves, FewShape<T, DH>::lds, s, a, c.keys, c.splits, part);
+  if (e != hipSuccess || c.splits == 1) return e;
+  const int64_t rows = (int64_t)a.how.batch * a.how.n_head * a.how.n_q;
+  return start(heads_join_kernel<T, DH>, (rows + 3) / 4, 256, 0, s, a, c.splits, (const float*)part);
+}
+
+size_t stats_bytes(const zgr_attention& how) { return ((size_t)how.batch * how.n_head * 2 * (size_t)stat_rows(how.n_q) * 4 + 255) / 256 * 256; }
+int parts_of(const zgr_attention& how) { return how.batch * ((how.n_q + 32 * kQueryWaves - 1) / (32 * kQueryWaves)); }
 
 template <typename T, int DH> hipError_t backward(const AttentionArgs& a, hipStream_t s) {
-  float* dots = reinterpret_cast<float*>(a.workspace);
-  float* parts = a.how.bias && a.dbias ? reinterpret_cast<float*>(a.workspace + dots_bytes(a.how)) : nullptr;
-  const int64_t qblocks = (int64_t)((a.how.n_q + kBlock - 1) / kBlock) * a.how.n_head * a.how.batch, kblocks = (int64_t)((a.how.n_k + kBlock - 1) / kBlock) * a.how.n_kv_head * a.how.batch;
-  int lds = dq_lds<T, DH>(a.how);
-  if (hipError_t e = with_lds(heads_dq_kernel<T, DH>, lds); e != hipSuccess) return e;
-  if (qblocks) hipLaunchKernelGGL((heads_dq_kernel<T, DH>), dim3(blocks_for(qblocks)), dim3(64 * kWaves), lds, s, a, dots, parts);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  lds = dkv_lds<T, DH>(a.how);
-  if (hipError_t e = with_lds(heads_dkv_kernel<T, DH>, lds); e != hipSuccess) return e;
-  if (kblocks) hipLaunchKernelGGL((heads_dkv_kernel<T, DH>), dim3(blocks_for(kblocks)), dim3(64 * kWaves), lds, s, a, dots);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (parts) hipLaunchKernelGGL((heads_dbias_kernel<T>), dim3(a.how.n_head), dim3(1024), (2 * a.how.bias_reach + 1) * 4, s, a.how, parts, parts_of(a.how), (T*)a.dbias);
+  float* stats = reinterpret_cast<float*>(a.workspace);
+  float* parts = a.dbias ? reinterpret_cast<float*>(a.workspace + stats_bytes(a.how)) : nullptr;
+  hipError_t e = start(heads_dq_kernel<T, DH, kQueryWaves>, (blocks_of(a.how.n_q, 32 * kQueryWaves, a.how.n_head, a.how.batch) + 7) / 8 * 8, 64 * kQueryWaves, dq_lds<T, DH, kQueryWaves>(a.how), s, a, stats, parts);
+  if (e == hipSuccess) e = start(heads_dkv_kernel<T, DH, kKeyWaves>, (blocks_of(a.how.n_k, 32 * kKeyWaves, a.how.n_kv_head, a.how.batch) + 7) / 8 * 8, 64 * kKeyWaves, dkv_lds<T, DH>(a.how), s, a, stats);
+  if (e != hipSuccess || !parts) return e;
+  hipLaunchKernelGGL((heads_dbias_kernel<T>), dim3(a.how.n_head), dim3(1024), (2 * a.how.bias_reach + 1) * 4, s, a.how, parts, parts_of(a.how), (T*)a.dbias);
   return hipGetLastError();
 }
 
@@ -668,9 +1009,9 @@ int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
 
 }  // namespace
 
-size_t attention_workspace(const zgr_attention&) { return 256; }
+size_t attention_workspace(const zgr_attention& how) { return part_bytes(how, padded_dim(how.head_dim)); }
 size_t attention_backward_workspace(const zgr_attention& how) {
-  return dots_bytes(how) + (how.bias ? ((size_t)parts_of(how) * how.n_head * (2 * (size_t)how.bias_reach + 1) * 4 + 255) / 256 * 256 : 0);
+  return stats_bytes(how) + (how.bias ? ((size_t)parts_of(how) * how.n_head * (2 * (size_t)how.bias_reach + 1) * 4 + 255) / 256 * 256 : 0);
 }
 
 hipError_t launch_heads_forward(const AttentionArgs& a, hipStream_t s) {
