@@ -98,15 +98,19 @@ __device__ __forceinline__ float diagonal_sums(const float (&x)[16], int lane) {
 }
 __device__ __forceinline__ f32x16 zeros16() { return f32x16{}; }
 
-// first kind: tile += rows row0 .. row0 + 31 of LDS x own
+// first kind: rows row0 .. row0 + 31 of LDS x own.  The reads are all issued before the first product, which left to itself the compiler takes in pairs, each with a wait of its own.
 template <typename T, int DH> __device__ __forceinline__ f32x16 rows_product(const unsigned char* lds, int row0, const Own<T, DH>& own, int l32, int half) {
   constexpr int bytes = DH * (int)sizeof(T);
   f32x16 acc = zeros16();
   const unsigned char* row = lds + (row0 + l32) * bytes;
   const int t = turn_of<T, DH>(l32);
   if constexpr (sizeof(T) == 2) {
+    bf16x8 a[DH / 16];
 #pragma unroll
-    for (int s = 0; s < DH / 16; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(row + (((2 * s + half) ^ t) << 4)), own.f[s], acc, 0, 0, 0);
+    for (int s = 0; s < DH / 16; ++s) a[s] = *reinterpret_cast<const bf16x8*>(row + (((2 * s + half) ^ t) << 4));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s], own.f[s], acc, 0, 0, 0);
   } else {
 #pragma unroll
     for (int s = 0; s < DH / 8; ++s) {
@@ -126,34 +130,70 @@ template <> struct Tile<float> { float w[16]; };
 __device__ __forceinline__ void put_pair(Tile<bf16_bits>& t, int v, float a, float b) { t.w[v / 2] = pack_bf16(a, b); }
 __device__ __forceinline__ void put_pair(Tile<float>& t, int v, float a, float b) { t.w[v] = a; t.w[v + 1] = b; }
 
-// second kind: acc[f] (entries 32 f ..) += (rows row0 .. row0 + 31 of LDS)^T x tile
-template <typename T, int DH> __device__ __forceinline__ void columns_product(f32x16 (&acc)[DH / 32], const unsigned char* lds, int row0, const Tile<T>& tile, int lane) {
-  constexpr int bytes = DH * (int)sizeof(T);
+// Columns of 32 rows of LDS, for the second kind.  bf16: 16 lanes receive the columns of a piece of 4 rows of 16 entries.  Written as one block with its wait: behind the builtin the
+// compiler waits for every transfer to LDS that is on its way (at the builtin's first use 2 x 2047 tokens, 32 heads of 128 took 760 us backward and 165 forward).  It goes where
+// products of the first kind have just been issued, which run meanwhile.
+template <typename T, int DH> struct Columns;
+template <int DH> struct Columns<bf16_bits, DH> { u32x2_t lo[2][DH / 32], hi[2][DH / 32]; };
+template <int DH> struct Columns<float, DH> { const unsigned char* at[4]; };
+
+template <typename T, int DH> __device__ __forceinline__ void load_columns(Columns<T, DH>& c, const unsigned char* lds, int row0, int lane) {
+  constexpr int bytes = DH * (int)sizeof(T), F = DH / 32;
   const int half = lane >> 5, l32 = lane & 31;
   if constexpr (sizeof(T) == 2) {
+#if defined(__HIP_DEVICE_COMPILE__)
     const int i16 = lane & 15, piece = ((lane & 16) >> 3) + ((i16 & 3) >> 1), down = (i16 >> 2) + 4 * half;
-    const unsigned char* at = lds + (row0 + down) * bytes + (i16 & 1) * 8;
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds + (uint32_t)((row0 + down) * bytes + (i16 & 1) * 8);
     const int t0 = turn_of<T, DH>(down), t1 = turn_of<T, DH>(down + 8);
+    uint32_t a[F], b[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      a[f] = at + (uint32_t)(((4 * f + piece) ^ t0) << 4);
+      b[f] = at + (uint32_t)(((4 * f + piece) ^ t1) << 4);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (F == 1)
+      asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5 offset:512\n\tds_read_b64_tr_b16 %2, %4 offset:1024\n\tds_read_b64_tr_b16 %3, %5 offset:1536\n\ts_waitcnt lgkmcnt(0)"
+                   : "=&v"(c.lo[0][0]), "=&v"(c.hi[0][0]), "=&v"(c.lo[1][0]), "=&v"(c.hi[1][0]) : "v"(a[0]), "v"(b[0]) : "memory");
+    else if constexpr (F == 2)
+      asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9 offset:1024\n\tds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11 offset:1024\n\t"
+                   "ds_read_b64_tr_b16 %4, %8 offset:2048\n\tds_read_b64_tr_b16 %5, %9 offset:3072\n\tds_read_b64_tr_b16 %6, %10 offset:2048\n\tds_read_b64_tr_b16 %7, %11 offset:3072\n\t"
+                   "s_waitcnt lgkmcnt(0)"
+                   : "=&v"(c.lo[0][0]), "=&v"(c.hi[0][0]), "=&v"(c.lo[0][1]), "=&v"(c.hi[0][1]), "=&v"(c.lo[1][0]), "=&v"(c.hi[1][0]), "=&v"(c.lo[1][1]), "=&v"(c.hi[1][1])
+                   : "v"(a[0]), "v"(b[0]), "v"(a[F > 1 ? 1 : 0]), "v"(b[F > 1 ? 1 : 0]) : "memory");
+    else
+      asm volatile("ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %17 offset:2048\n\tds_read_b64_tr_b16 %2, %18\n\tds_read_b64_tr_b16 %3, %19 offset:2048\n\t"
+                   "ds_read_b64_tr_b16 %4, %20\n\tds_read_b64_tr_b16 %5, %21 offset:2048\n\tds_read_b64_tr_b16 %6, %22\n\tds_read_b64_tr_b16 %7, %23 offset:2048\n\t"
+                   "ds_read_b64_tr_b16 %8, %16 offset:4096\n\tds_read_b64_tr_b16 %9, %17 offset:6144\n\tds_read_b64_tr_b16 %10, %18 offset:4096\n\tds_read_b64_tr_b16 %11, %19 offset:6144\n\t"
+                   "ds_read_b64_tr_b16 %12, %20 offset:4096\n\tds_read_b64_tr_b16 %13, %21 offset:6144\n\tds_read_b64_tr_b16 %14, %22 offset:4096\n\tds_read_b64_tr_b16 %15, %23 offset:6144\n\t"
+                   "s_waitcnt lgkmcnt(0)"
+                   : "=&v"(c.lo[0][0]), "=&v"(c.hi[0][0]), "=&v"(c.lo[0][1]), "=&v"(c.hi[0][1]), "=&v"(c.lo[0][2]), "=&v"(c.hi[0][2]), "=&v"(c.lo[0][3]), "=&v"(c.hi[0][3]),
+                     "=&v"(c.lo[1][0]), "=&v"(c.hi[1][0]), "=&v"(c.lo[1][1]), "=&v"(c.hi[1][1]), "=&v"(c.lo[1][2]), "=&v"(c.hi[1][2]), "=&v"(c.lo[1][3]), "=&v"(c.hi[1][3])
+                   : "v"(a[0]), "v"(b[0]), "v"(a[F > 1 ? 1 : 0]), "v"(b[F > 1 ? 1 : 0]), "v"(a[F > 2 ? 2 : 0]), "v"(b[F > 2 ? 2 : 0]), "v"(a[F > 3 ? 3 : 0]), "v"(b[F > 3 ? 3 : 0]) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c.at[i] = lds + (row0 + 4 * half) * bytes + (((l32 >> 2) ^ (4 * half + i)) << 4) + (l32 & 3) * 4;
+  }
+}
+
+// second kind: acc[f] (entries 32 f ..) += columns x tile
+template <typename T, int DH> __device__ __forceinline__ void columns_product(f32x16 (&acc)[DH / 32], const Columns<T, DH>& c, const Tile<T>& tile) {
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       const bf16x8 b = __builtin_bit_cast(bf16x8, u32x4_t{tile.w[4 * ks], tile.w[4 * ks + 1], tile.w[4 * ks + 2], tile.w[4 * ks + 3]});
 #pragma unroll
-      for (int f = 0; f < DH / 32; ++f) {
-        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-        const u32x2_t lo = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)const_cast<unsigned char*>(at + 16 * ks * bytes + (((4 * f + piece) ^ t0) << 4))));
-        const u32x2_t hi = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)const_cast<unsigned char*>(at + (16 * ks + 8) * bytes + (((4 * f + piece) ^ t1) << 4))));
-        acc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4_t{lo[0], lo[1], hi[0], hi[1]}), b, acc[f], 0, 0, 0);
-      }
+      for (int f = 0; f < DH / 32; ++f)
+        acc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4_t{c.lo[ks][f][0], c.lo[ks][f][1], c.hi[ks][f][0], c.hi[ks][f][1]}), b, acc[f], 0, 0, 0);
     }
   } else {
-    const unsigned char* at[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) at[i] = lds + (row0 + 4 * half) * bytes + (((l32 >> 2) ^ (4 * half + i)) << 4) + (l32 & 3) * 4;
 #pragma unroll
     for (int v = 0; v < 16; ++v)
 #pragma unroll
       for (int f = 0; f < DH / 32; ++f)
-        acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at[v & 3] + (8 * (v >> 2) + (v & 3)) * bytes + f * 128), tile.w[v], acc[f], 0, 0, 0);
+        acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(c.at[v & 3] + (8 * (v >> 2) + (v & 3)) * DH * 4 + f * 128), tile.w[v], acc[f], 0, 0, 0);
   }
 }
 
@@ -186,15 +226,34 @@ template <typename T, int DH> __device__ __forceinline__ void columns_exactly(f3
 
 // Rows first .. first + ROWS - 1 of a head of two operands, one behind the other, straight into LDS; rows past `last` repeat it (whoever reads them hides them).  NW waves share
 // the pieces of 1 KiB evenly.
+// Where all rows are there and a row's offset among the few of one transfer fits 32 bits, its address is a scalar and one register, which differ from transfer to transfer by
+// scalar arithmetic and an exclusive or: ten vector instructions fewer a transfer, which a wave with no other beside it has nothing to hide behind.
 template <typename T, int DH, int ROWS, int NW>
 __device__ __forceinline__ void stage_rows(unsigned char* lds, const T* base0, int64_t token0, const T* base1, int64_t token1, int first, int last, int dim, int wave, int lane) {
-  constexpr int bytes = DH * (int)sizeof(T), per = 1024 / bytes, pieces = ROWS * bytes / 1024;
+  constexpr int bytes = DH * (int)sizeof(T), per = 1024 / bytes, pieces = ROWS * bytes / 1024, N = 2 * pieces / NW;
   static_assert(2 * pieces % NW == 0, "whole instructions");
+  const int down = lane * 16 / bytes, place = lane & (bytes / 16 - 1);
+  const uint64_t most = (uint64_t)1 << 30;
+  if (dim == DH && first + ROWS - 1 <= last && (uint64_t)token0 * (per * sizeof(T)) < most && (uint64_t)token1 * (per * sizeof(T)) < most) {
+    const uint32_t turned = (uint32_t)((place ^ turn_of<T, DH>(down)) << 4), off0 = (uint32_t)down * (uint32_t)(token0 * (int64_t)sizeof(T)), off1 = (uint32_t)down * (uint32_t)(token1 * (int64_t)sizeof(T));
 #pragma unroll
-  for (int i = 0; i < 2 * pieces / NW; ++i) {
+    for (int i = 0; i < N; ++i) {
+      const int piece = i * NW + wave;
+      const bool second = piece >= pieces;
+      const int row = (second ? piece - pieces : piece) * per;      // turn_of picks bits: of row + down it is the exclusive or of both
+      const unsigned char* from = reinterpret_cast<const unsigned char*>((second ? base1 : base0) + (int64_t)(first + row) * (second ? token1 : token0));
+      const uint32_t off = (turned ^ (uint32_t)(turn_of<T, DH>(row) << 4)) + (second ? off1 : off0);
+#if defined(__HIP_DEVICE_COMPILE__)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(from + off), (__attribute__((address_space(3))) void*)(lds + piece * 1024), 16, 0, 0);
+#endif
+    }
+    return;
+  }
+#pragma unroll 2
+  for (int i = 0; i < N; ++i) {
     const int piece = i * NW + wave;
     const bool second = piece >= pieces;
-    const int r = (second ? piece - pieces : piece) * per + lane * 16 / bytes, c = (lane & (bytes / 16 - 1)) ^ turn_of<T, DH>(r);
+    const int r = (second ? piece - pieces : piece) * per + down, c = place ^ turn_of<T, DH>(r);
     const T* src = (second ? base1 : base0) + (int64_t)min(first + r, last) * (second ? token1 : token0) + c * (16 / (int)sizeof(T));
     if (dim != DH) src = c * (16 / (int)sizeof(T)) < dim ? src : reinterpret_cast<const T*>(kZeros);
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -274,6 +333,19 @@ __host__ __device__ inline int64_t stat_rows(int n_q) { return ((int64_t)n_q + k
 // which w and w + 4 share a SIMD, the upper four take their queries in reverse order.
 template <int NW> __device__ __forceinline__ int group_of(int wave, int causal) { return NW == 8 && causal && wave >= 4 ? 11 - wave : wave; }
 
+// The maximum that the exponentials are taken against follows a tile's only where that is more than 2^8 times as large: sums and probabilities of up to 2^8 keep their relative
+// rounding, and past the first tiles nothing is rescaled (with the maximum itself one of 32 rows moves it in 40 % of the tiles after 64 of them).
+template <int DH> __device__ __forceinline__ void raise_maximum(float top, float& mx, float& lsum, f32x16 (&o)[DH / 32]) {
+  if (__builtin_amdgcn_ballot_w64(top > mx + 8.0f) == 0) return;
+  const float mnew = fmaxf(mx, top), corr = mnew == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mx - mnew);
+  mx = mnew;
+  lsum *= corr;
+#pragma unroll
+  for (int f = 0; f < DH / 32; ++f)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[f][v] *= corr;
+}
+
 // ------------------------------------------------------------------------------------------------ forward
 template <typename T, int DH, int NW>
 __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs a) {
@@ -330,6 +402,8 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
         if (k0 >= wave_kend) break;
         if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, qi < sq.n_q);      // so that it takes no registers beside columns_exactly's
         const f32x16 s = rows_product<T, DH>(K, kl, q, l32, half);
+        Columns<T, DH> cols;
+        if (!careful) load_columns<T, DH>(cols, V, kl, lane);
         const bool whole = k0 + 31 < sq.n_k && (!causal || k0 + 31 <= pos0);                     // every query of the wave sees every key of the tile
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;           // the tile has more than one relative position within reach
         float x[16], by = scale, top, flat = 0.f;          // score = by x + flat
@@ -357,8 +431,8 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
         top = x[0];
 #pragma unroll
         for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
-        const float mnew = fmaxf(mx, __builtin_fmaf(max_of_halves(top), by, flat)), msafe = mnew == -INFINITY ? 0.f : mnew, less = flat - msafe;
-        const float corr = __builtin_amdgcn_exp2f(mx - msafe);
+        raise_maximum<DH>(__builtin_fmaf(max_of_halves(top), by, flat), mx, lsum, o);
+        const float msafe = mx == -INFINITY ? 0.f : mx, less = flat - msafe;
         float sum = 0.f;
         Tile<T> p;
 #pragma unroll
@@ -368,16 +442,12 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
           sum += x[v] + x[v + 1];
           put_pair(p, v, x[v], x[v + 1]);
         }
-        lsum = __builtin_fmaf(lsum, corr, sum);
-        mx = mnew;
-        if (__builtin_amdgcn_ballot_w64(corr != 1.0f) != 0) {
-#pragma unroll
-          for (int f = 0; f < DH / 32; ++f)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[f][v] *= corr;
-        }
+        lsum += sum;
         if (careful && !whole) columns_exactly<T, DH>(o, V, kl, x, seen, lane);
-        else columns_product<T, DH>(o, V, kl, p, lane);
+        else {
+          if (careful) load_columns<T, DH>(cols, V, kl, lane);
+          columns_product<T, DH>(o, cols, p);
+        }
       }
     }
     transfers_upto<0>();                                   // LDS is another's after the last wave
@@ -402,204 +472,294 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
 }
 
 // ------------------------------------------------------------------------------------------------ forward, few queries over many keys
-// Bound by the bytes of K and V: the 32 columns of a wave are the queries of all the query heads that share a K/V head, so that those are read once, and every wave walks
-// keys of its own (every kFewWaves-th tile of a chunk), staged for it alone: no barriers, and 2 RING tiles of a block on their way.  Chunks of long sequences are blocks of their own, whose
-// sums heads_join_kernel puts together.
-constexpr int kFewWaves = 2;
+// Bound by the bytes of K and V: the 32 columns of a wave are the queries of all the query heads that share a K/V head, so that those are read once.  All tiles of 32 keys, of every
+// sequence, K/V head and 32 columns (an item), stand in one line, and every wave takes an equal run of it, whatever the lengths are: the chip is filled once, with one wave a block and
+// tiles staged for it alone, so there are no barriers, and the next tile is on its way while this one is worked on.  A wave writes the rows of an item that lies in its run, and
+// leaves the sums of its share of one that doesn't (at most two: where the run begins and where it ends) to heads_join_kernel.
+// (Blocks of equal chunks of a sequence: 16 sequences of 1000 to 16384 tokens 195 us, in chunks of 1024 keys, of which the last of three rounds of blocks was a third full, and
+// more in smaller ones.)
 template <typename T, int DH> struct FewShape {
   static constexpr int row = DH * (int)sizeof(T), tile = 2 * 32 * row, ring = tile <= 8192 ? 4 : 2, per = tile / 1024;
-  static constexpr int join = kFewWaves * (DH * 33 + 64) * 4;      // the waves' results
-  static constexpr int lds = kFewWaves * ring * tile > join ? kFewWaves * ring * tile : join;
 };
+constexpr int kFewBatch = 1024;                             // sequences whose tiles a wave counts for itself
 __device__ __forceinline__ void reads_done() {              // this wave's reads of LDS have returned
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #endif
 }
+// Tiles of each item of a sequence; one that sees no key has one all the same, which writes its zeros.
+__device__ __forceinline__ int tiles_of(const zgr_attention& how, const Sequence& sq) {
+  int kend = sq.n_q > 0 ? sq.n_k : 0;
+  if (how.causal) kend = min(kend, sq.start + sq.n_q);
+  return max(1, (kend + 31) / 32);
+}
+// Of worker g of `workers`: its first tile of `total`.
+__device__ __forceinline__ int64_t first_tile(int64_t g, int64_t workers, int64_t total) { return g * total / workers; }
+struct FewWork { int workers, row_blocks, rows; };          // rows: of an item, at most 32
 
-// part: [splits][rows][DH] sums and then [splits][rows][2] maxima (log2) and sums of exponentials, rows = batch n_head n_q; splits == 1: none
+// part: [workers][2][rows][DH] sums and then [workers][2][rows][2] maxima (log2) and sums of exponentials; ahead: [batch + 1], the tiles in front of each sequence.
+// even = 0: a worker is an item.
 template <typename T, int DH>
-__global__ void __launch_bounds__(64 * kFewWaves, DH * sizeof(T) >= 256 ? 1 : 2) heads_few_kernel(AttentionArgs a, int chunk, int splits, float* __restrict__ part) {
+__global__ void __launch_bounds__(64, DH * sizeof(T) >= 256 ? 1 : 2) heads_few_kernel(AttentionArgs a, FewWork w, int even, float* __restrict__ part, int64_t* __restrict__ ahead) {
   using Sh = FewShape<T, DH>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int group = how.n_head / how.n_kv_head, rows = group * how.n_q, row_blocks = (rows + 31) / 32;
-  const int split = (int)(blockIdx.x % (unsigned)splits);
-  const int64_t item = blockIdx.x / (unsigned)splits;
-  const int rb = (int)(item % row_blocks), hk = (int)(item / row_blocks % how.n_kv_head), b = (int)(item / row_blocks / how.n_kv_head);
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  const Sequence sq = sequence_of(how, b);
-  const int r = rb * 32 + l32, head = min(r, rows - 1) / how.n_q, i = min(r, rows - 1) - head * how.n_q, h = hk * group + head;
-  const bool valid = r < rows && i < sq.n_q;
-  // positions of the block's queries: of one head, or all
-  const int first_row = rb * 32, last_row = min(rows, first_row + 32) - 1;
-  const bool one_head = first_row / how.n_q == last_row / how.n_q;
-  const int i_low = one_head ? first_row % how.n_q : 0, i_high = min(one_head ? last_row % how.n_q : how.n_q - 1, sq.n_q - 1);
-  const int pos = sq.start + i, pos_low = sq.start + i_low, pos_high = sq.start + i_high;
+  const int group = how.n_head / how.n_kv_head, rows = group * how.n_q, items = w.row_blocks * how.n_kv_head;      // items of a sequence
+  const int lane = threadIdx.x, l32 = lane & 31, half = lane >> 5;
+  struct Cursor { int b, item, tile, tiles; };
+  Cursor here{0, 0, 0, 0};
+  int count;
+  if (even) {
+    // the tiles of all sequences, and the place of this worker's first
+    int64_t total = 0;
+    for (int b0 = 0; b0 < how.batch; b0 += 64) {
+      const int b = b0 + lane;
+      int64_t n = b < how.batch ? (int64_t)tiles_of(how, sequence_of(how, b)) * items : 0;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) n += __shfl_xor(n, o, 64);
+      total += n;
+    }
+    const int64_t workers = min((int64_t)w.workers, total);      // every one of them has a tile
+    if (blockIdx.x >= workers) return;
+    const int64_t from = first_tile(blockIdx.x, workers, total);
+    count = uniform_of((int)(first_tile(blockIdx.x + 1, workers, total) - from));
+    int64_t before = 0;
+    bool found = false;
+    for (int b0 = 0; b0 < how.batch; b0 += 64) {
+      const int b = b0 + lane, tiles = b < how.batch ? tiles_of(how, sequence_of(how, b)) : 0;
+      const int64_t own = (int64_t)tiles * items;
+      int64_t upto = own;                                   // and those of the lanes below
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) { const int64_t v = __shfl_up(upto, o, 64); if (lane >= o) upto += v; }
+      if (blockIdx.x == 0 && b < how.batch) ahead[b] = before + upto - own;
+      const uint64_t beyond = __builtin_amdgcn_ballot_w64(b < how.batch && before + upto > from);
+      if (!found && beyond) {
+        const int at = __builtin_ctzll(beyond);
+        here.b = b0 + at;
+        here.tiles = __shfl(tiles, at, 64);
+        const int64_t in = from - (before + __shfl(upto - own, at, 64));
+        here.item = (int)(in / here.tiles), here.tile = (int)(in - (int64_t)here.item * here.tiles);
+        found = true;
+      }
+      before += __shfl(upto, 63, 64);
+    }
+    if (blockIdx.x == 0 && lane == 0) ahead[how.batch] = total;
+    here.b = uniform_of(here.b), here.item = uniform_of(here.item), here.tile = uniform_of(here.tile), here.tiles = uniform_of(here.tiles);
+  } else {
+    here.b = (int)(blockIdx.x / (unsigned)items), here.item = (int)(blockIdx.x % (unsigned)items);
+    here.tiles = uniform_of(tiles_of(how, sequence_of(how, here.b)));
+    count = here.tiles;
+  }
+  auto next = [&](Cursor& c) {                              // past the last tile of all it stays there
+    if (++c.tile < c.tiles) return;
+    if (c.item + 1 < items) { ++c.item; c.tile = 0; return; }
+    if (c.b + 1 < how.batch) { ++c.b; c.item = 0; c.tile = 0; c.tiles = uniform_of(tiles_of(how, sequence_of(how, c.b))); return; }
+    c.tile = c.tiles - 1;
+  };
+  Cursor later = here;
+  int staged = 0;
+  auto stage = [&]() {
+    const int hk = later.item / w.row_blocks, last = uniform_of(max(sequence_of(how, later.b).n_k - 1, 0));
+    stage_rows<T, DH, 32, 1>(lds + staged % Sh::ring * Sh::tile, row_at<T>(a.k, later.b, 0, hk), a.k.token, row_at<T>(a.v, later.b, 0, hk), a.v.token, min(later.tile * 32, last), last, how.head_dim, 0, lane);
+    ++staged;
+    next(later);
+  };
+#pragma unroll
+  for (int n = 0; n < Sh::ring - 1; ++n) stage();
+  const float scale = how.scale * kLog2e;
   const int causal = how.causal, reach = how.bias_reach;
   const bool biased = how.bias != nullptr;
-  int kend = i_low <= i_high ? sq.n_k : 0;
-  if (causal) kend = min(kend, pos_high + 1);
-  const int kbegin = split * chunk;
-  kend = min(kend, kbegin + chunk);
-  const int tiles = kend > kbegin ? (kend - kbegin + 31) / 32 : 0, mine = tiles > wave ? (tiles - wave + kFewWaves - 1) / kFewWaves : 0;
-  const T* kbase = row_at<T>(a.k, b, 0, hk);
-  const T* vbase = row_at<T>(a.v, b, 0, hk);
-  unsigned char* ring = lds + wave * Sh::ring * Sh::tile;
-  auto stage = [&](int n) {                                 // this wave's n-th tile; past the last one its last row again
-    stage_rows<T, DH, 32, 1>(ring + n % Sh::ring * Sh::tile, kbase, a.k.token, vbase, a.v.token, min(kbegin + (n * kFewWaves + wave) * 32, sq.n_k - 1), sq.n_k - 1, how.head_dim, 0, lane);
-  };
-  const float scale = how.scale * kLog2e;
-  auto bias_at = [&](int delta) {                           // a column's own head: looked up where the tables lie
-    const int bucket = how.bias_map[min(max(delta, -reach), reach) + reach];
-    return bucket >= 0 && bucket < how.bias_buckets ? as_float(((const T*)how.bias)[(int64_t)bucket * how.n_head + h]) * kLog2e : __uint_as_float(0x7FC00000u);
-  };
-  Own<T, DH> q;
-  f32x16 o[DH / 32];
-  float mx, lsum, flat_low = 0.f, flat_high = 0.f;
-  auto pass = [&](auto again) -> bool {
-    constexpr bool careful = decltype(again)::value;
-    if (mine)
+  int done = 0;
+  while (done < count) {                                    // an item, or what of it lies in this worker's run
+    Sequence sq = sequence_of(how, here.b);
+    sq.n_q = uniform_of(sq.n_q), sq.n_k = uniform_of(sq.n_k), sq.start = uniform_of(sq.start);
+    const int rb = here.item % w.row_blocks, hk = here.item / w.row_blocks, b = here.b;
+    const int r = rb * 32 + l32, head = min(r, rows - 1) / how.n_q, i = min(r, rows - 1) - head * how.n_q, h = hk * group + head;
+    const bool valid = r < rows && i < sq.n_q;
+    // positions of the item's queries: of one head, or all
+    const int first_row = rb * 32, last_row = min(rows, first_row + 32) - 1;
+    const bool one_head = first_row / how.n_q == last_row / how.n_q;
+    const int i_low = one_head ? first_row % how.n_q : 0, i_high = min(one_head ? last_row % how.n_q : how.n_q - 1, sq.n_q - 1);
+    const int pos = sq.start + i, pos_low = sq.start + i_low, pos_high = sq.start + i_high;
+    int kend = i_low <= i_high ? sq.n_k : 0;
+    if (causal) kend = min(kend, pos_high + 1);
+    auto bias_at = [&](int delta) {                         // a column's own head: looked up where the tables lie
+      const int bucket = how.bias_map[min(max(delta, -reach), reach) + reach];
+      return bucket >= 0 && bucket < how.bias_buckets ? as_float(((const T*)how.bias)[(int64_t)bucket * how.n_head + h]) * kLog2e : __uint_as_float(0x7FC00000u);
+    };
+    const int from = here.tile, share = min(here.tiles - from, count - done);
+    Own<T, DH> q;
+    f32x16 o[DH / 32];
+    float mx, lsum, flat_low = 0.f, flat_high = 0.f;
+    load_own<T, DH>(q, row_at<T>(a.q, b, i, h), half, how.head_dim, valid);
+    if (biased) { flat_low = bias_at(-reach); flat_high = bias_at(reach); }
+    auto pass = [&](auto again) -> bool {
+      constexpr bool careful = decltype(again)::value;
 #pragma unroll
-      for (int n = 0; n < Sh::ring - 1; ++n) stage(n);
-    if (!careful) {
-      load_own<T, DH>(q, row_at<T>(a.q, b, i, h), half, how.head_dim, valid);
-      if (biased) { flat_low = bias_at(-reach); flat_high = bias_at(reach); }
-    }
+      for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
+      mx = -INFINITY, lsum = 0.f;
+      for (int n = 0; n < share; ++n) {
+        const int k0 = (from + n) * 32;
+        const unsigned char* K = lds + (done + n) % Sh::ring * Sh::tile;
+        if (careful) {                                      // out of turn: in the first place of the ring, whose transfers are made again afterwards
+          K = lds;
+          reads_done();
+          transfers_upto<0>();
+          stage_rows<T, DH, 32, 1>(lds, row_at<T>(a.k, b, 0, hk), a.k.token, row_at<T>(a.v, b, 0, hk), a.v.token, min(k0, max(sq.n_k - 1, 0)), max(sq.n_k - 1, 0), how.head_dim, 0, lane);
+          transfers_upto<0>();
+          load_own<T, DH>(q, row_at<T>(a.q, b, i, h), half, how.head_dim, valid);
+        } else {
+          reads_done();                                     // of the tile whose place the next transfers take
+          stage();
+          transfers_upto<Sh::per * (Sh::ring - 1)>();
+        }
+        const unsigned char* V = K + Sh::tile / 2;
+        if (k0 >= kend) continue;
+        const f32x16 s = rows_product<T, DH>(K, 0, q, l32, half);
+        Columns<T, DH> cols;
+        if (!careful) load_columns<T, DH>(cols, V, 0, lane);
+        const bool whole = k0 + 31 < sq.n_k && (!causal || k0 + 31 <= pos_low);
+        const bool near = biased && k0 + 31 - pos_low > -reach && k0 - pos_high < reach;
+        float x[16];
+        if (near) {
 #pragma unroll
-    for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
-    mx = -INFINITY, lsum = 0.f;
-    for (int n = 0; n < mine; ++n) {
-      reads_done();                                         // of the tile whose place the next transfers take
-      stage(n + Sh::ring - 1);
-      transfers_upto<Sh::per * (Sh::ring - 1)>();
-      const unsigned char* K = ring + n % Sh::ring * Sh::tile;
-      const unsigned char* V = K + Sh::tile / 2;
-      const int k0 = kbegin + (n * kFewWaves + wave) * 32;
-      if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, i, h), half, how.head_dim, valid);
-      const f32x16 s = rows_product<T, DH>(K, 0, q, l32, half);
-      const bool whole = k0 + 31 < sq.n_k && (!causal || k0 + 31 <= pos_low);
-      const bool near = biased && k0 + 31 - pos_low > -reach && k0 - pos_high < reach;
-      float x[16];
-      const float flat = k0 < pos_low ? flat_low : flat_high;
+          for (int v = 0; v < 16; ++v) x[v] = bias_at(k0 + 8 * (v >> 2) + 4 * half + (v & 3) - pos);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, flat);
-      if (near) {
-        float by[16];
+          for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, x[v]);
+        } else {
+          const float flat = k0 < pos_low ? flat_low : flat_high;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) by[v] = bias_at(k0 + 8 * (v >> 2) + 4 * half + (v & 3) - pos);
+          for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, flat);
+        }
+        uint32_t seen = 0xFFFF;
+        if (!whole) {
+          seen = 0;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = __builtin_fmaf(s[v], scale, by[v]);
-      }
-      uint32_t seen = 0xFFFF;
-      if (!whole) {
-        seen = 0;
+          for (int v = 0; v < 16; ++v) {
+            const int key = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
+            const bool on = key < sq.n_k && (!causal || key <= pos);
+            seen |= (uint32_t)on << v;
+            x[v] = on ? x[v] : -INFINITY;
+          }
+        }
+        float top = x[0];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int key = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
-          const bool on = key < sq.n_k && (!causal || key <= pos);
-          seen |= (uint32_t)on << v;
-          x[v] = on ? x[v] : -INFINITY;
+        for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+        raise_maximum<DH>(max_of_halves(top), mx, lsum, o);
+        const float msafe = mx == -INFINITY ? 0.f : mx;
+        float sum = 0.f;
+        Tile<T> p;
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) {
+          x[v] = __builtin_amdgcn_exp2f(x[v] - msafe);
+          x[v + 1] = __builtin_amdgcn_exp2f(x[v + 1] - msafe);
+          sum += x[v] + x[v + 1];
+          put_pair(p, v, x[v], x[v + 1]);
+        }
+        lsum += sum;
+        if (careful && !whole) columns_exactly<T, DH>(o, V, 0, x, seen, lane);
+        else {
+          if (careful) load_columns<T, DH>(cols, V, 0, lane);
+          columns_product<T, DH>(o, cols, p);
         }
       }
-      float top = x[0];
-#pragma unroll
-      for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
-      const float mnew = fmaxf(mx, max_of_halves(top)), msafe = mnew == -INFINITY ? 0.f : mnew;
-      const float corr = __builtin_amdgcn_exp2f(mx - msafe);
-      float sum = 0.f;
-      Tile<T> p;
-#pragma unroll
-      for (int v = 0; v < 16; v += 2) {
-        x[v] = __builtin_amdgcn_exp2f(x[v] - msafe);
-        x[v + 1] = __builtin_amdgcn_exp2f(x[v + 1] - msafe);
-        sum += x[v] + x[v + 1];
-        put_pair(p, v, x[v], x[v + 1]);
-      }
-      lsum = __builtin_fmaf(lsum, corr, sum);
-      mx = mnew;
+      if (careful) return false;
+      bool bad = false;
 #pragma unroll
       for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[f][v] *= corr;
-      if (careful && !whole) columns_exactly<T, DH>(o, V, 0, x, seen, lane);
-      else columns_product<T, DH>(o, V, 0, p, lane);
+        for (int v = 0; v < 16; ++v) bad |= !finite(o[f][v]);
+      return __builtin_amdgcn_ballot_w64(bad && valid) != 0;
+    };
+    const bool begins = from == 0, ends = from + share == here.tiles, again = pass(std::false_type());
+    done += share;
+    here.tile += share - 1;
+    next(here);
+    if (again) {
+      pass(std::true_type());
+      reads_done();                                         // the first place of the ring has been used: the tiles that were on their way once more
+      later = here;
+      staged = done;
+#pragma unroll
+      for (int n = 0; n < Sh::ring - 1; ++n) stage();
     }
-    transfers_upto<0>();
-    if (careful) return false;
-    bool bad = false;
+    lsum = both_halves(lsum);
+    const bool none = i >= sq.n_q || lsum == 0.f;
+    if (r < rows && begins && ends) {
+      if (none)
 #pragma unroll
-    for (int f = 0; f < DH / 32; ++f)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) bad |= !finite(o[f][v]);
-    return __builtin_amdgcn_ballot_w64(bad && valid) != 0;
-  };
-  if (pass(std::false_type())) pass(std::true_type());
-  lsum = both_halves(lsum);
-  __syncthreads();
-  float* joined = reinterpret_cast<float*>(lds);            // [waves][DH][33], then [waves][32][2]
-  float* stats = joined + kFewWaves * DH * 33;
-#pragma unroll
-  for (int f = 0; f < DH / 32; ++f)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) joined[(wave * DH + 32 * f + 8 * (v >> 2) + 4 * half + (v & 3)) * 33 + l32] = o[f][v];
-  if (half == 0) { stats[(wave * 32 + l32) * 2] = mx; stats[(wave * 32 + l32) * 2 + 1] = lsum; }
-  __syncthreads();
-  const int64_t all_rows = (int64_t)how.batch * how.n_head * how.n_q;
-  for (int at = tid; at < min(32, rows - first_row) * DH; at += 64 * kFewWaves) {
-    const int rr = at / DH, c = at % DH, hh = hk * group + (first_row + rr) / how.n_q, ii = (first_row + rr) % how.n_q;
-    const float m0 = stats[rr * 2], m1 = stats[(32 + rr) * 2], m = fmaxf(m0, m1), safe = m == -INFINITY ? 0.f : m;
-    const float w0 = __builtin_amdgcn_exp2f(m0 - safe), w1 = __builtin_amdgcn_exp2f(m1 - safe);
-    const float v = joined[c * 33 + rr] * w0 + joined[(DH + c) * 33 + rr] * w1, l = stats[rr * 2 + 1] * w0 + stats[(32 + rr) * 2 + 1] * w1;
-    const int64_t row = ((int64_t)b * how.n_head + hh) * how.n_q + ii;
-    if (splits == 1) {
-      const bool none = ii >= sq.n_q || l == 0.f;
-      if (c < how.head_dim) put_float(none ? 0.f : v / l, const_cast<T*>(row_at<T>(a.out, b, ii, hh)) + c);
-      if (c == 0) a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-    } else {
-      if (m != -INFINITY) part[((int64_t)split * all_rows + row) * DH + c] = v;      // not read otherwise
-      if (c == 0) {
-        float* st = part + (int64_t)splits * all_rows * DH + ((int64_t)split * all_rows + row) * 2;
-        st[0] = ii >= sq.n_q ? -INFINITY : m;
-        st[1] = l;
+        for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
+      store_columns<T, DH>(const_cast<T*>(row_at<T>(a.out, b, i, h)), o, none ? 0.f : 1.0f / lsum, half, how.head_dim);
+      if (half == 0) a.lse[((int64_t)b * how.n_head + h) * how.n_q + i] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(lsum)) * kLn2;
+    } else if (r < rows) {
+      const int64_t row = ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * w.rows + l32;
+      if (half == 0) {
+        float* st = part + (int64_t)w.workers * 2 * w.rows * DH + row * 2;
+        st[0] = none ? -INFINITY : mx;
+        st[1] = none ? 0.f : lsum;
       }
+      if (!none) store_columns<float, DH>(part + row * DH, o, 1.0f, half, DH);      // not read otherwise
     }
   }
+  transfers_upto<0>();
 }
 
-// The chunks' sums of a row: a wave each.
+// The sums that several workers left of a row: a block each, every fourth worker to a wave.
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, int splits, const float* __restrict__ part) {
-  const zgr_attention& how = a.how;
-  const int64_t all_rows = (int64_t)how.batch * how.n_head * how.n_q, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= all_rows) return;
-  const int lane = threadIdx.x & 63;
-  const float* stats = part + (int64_t)splits * all_rows * DH;
-  float m = -INFINITY;
-  for (int s = lane; s < splits; s += 64) m = fmaxf(m, stats[((int64_t)s * all_rows + row) * 2]);
-  m = wave_max(m);
-  const int b = (int)(row / ((int64_t)how.n_head * how.n_q)), h = (int)(row / how.n_q % how.n_head), i = (int)(row % how.n_q);
+__global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, FewWork w, const float* __restrict__ part, const int64_t* __restrict__ ahead) {
   constexpr int PER = DH / 64 > 0 ? DH / 64 : 1;
+  __shared__ float tops[4], sums[4][64 * PER + 1];
+  const zgr_attention& how = a.how;
+  const int64_t row = blockIdx.x;
+  const int b = (int)(row / ((int64_t)how.n_head * how.n_q)), h = (int)(row / how.n_q % how.n_head), i = (int)(row % how.n_q), group = how.n_head / how.n_kv_head;
+  const int r = (h % group) * how.n_q + i, items = w.row_blocks * how.n_kv_head;
+  const int64_t total = ahead[how.batch], tiles = (ahead[b + 1] - ahead[b]) / items, first = ahead[b] + ((int64_t)(h / group) * w.row_blocks + r / 32) * tiles;
+  const int64_t workers = min((int64_t)w.workers, total), g0 = ((first + 1) * workers - 1) / total, g1 = ((first + tiles) * workers - 1) / total;      // the workers of its first and last tile
+  if (g0 == g1) return;                                     // which wrote it
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)(g1 - g0) + 1;
+  auto place = [&](int j) { return ((g0 + j) * 2 + (j == 0 ? 1 : 0)) * w.rows + r % 32; };
+  const float* stats = part + (int64_t)w.workers * 2 * w.rows * DH;
+  float m = -INFINITY;
+  for (int j = tid; j < n; j += 256) m = fmaxf(m, stats[place(j) * 2]);
+  m = wave_max(m);
+  if (lane == 0) tops[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   float o[PER] = {}, l = 0.f;
-  if (m != -INFINITY) {
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-      const int64_t at = (int64_t)s * all_rows + row;
-      const float ms = stats[at * 2], w = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - m);      // a chunk without a visible key left nothing to weigh
-      l += w * stats[at * 2 + 1];
+  for (int j0 = 0; j0 < n && m != -INFINITY; j0 += 256) {   // 64 workers' weights in the lanes: those of j0 + 4 lane + wave
+    const int mine = j0 + 4 * lane + wave;
+    float weight = 0.f;
+    if (mine < n) {
+      const float* st = stats + place(mine) * 2;
+      weight = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - m);      // one without a visible key left nothing to weigh
+      l += weight * st[1];
+    }
+    uint64_t left = __builtin_amdgcn_ballot_w64(weight != 0.f);
+    while (left) {                                          // those with a weight, eight at a time
+      float wt[8], x[8][PER];
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int c = lane * PER + j;
-        if (c < DH && w != 0.f) o[j] += w * part[at * DH + c];
+      for (int k = 0; k < 8; ++k) {
+        const int at = left ? __builtin_ctzll(left) : 0;
+        wt[k] = left ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), at)) : 0.f;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) x[k][c] = left && lane * PER < DH ? part[place(j0 + 4 * at + wave) * DH + lane * PER + c] : 0.f;
+        left &= left - 1;
       }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int c = 0; c < PER; ++c) o[c] = __builtin_fmaf(wt[k], x[k][c], o[c]);
     }
   }
-  const bool none = l == 0.f;
-  T* out = const_cast<T*>(row_at<T>(a.out, b, i, h));
+  l = wave_sum(l);
 #pragma unroll
-  for (int j = 0; j < PER; ++j)
-    if (lane * PER + j < how.head_dim) put_float(none ? 0.f : o[j] / l, out + lane * PER + j);
-  if (lane == 0) a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  for (int c = 0; c < PER; ++c) sums[wave][lane * PER + c] = o[c];
+  if (lane == 0) sums[wave][64 * PER] = l;
+  __syncthreads();
+  l = (sums[0][64 * PER] + sums[1][64 * PER]) + (sums[2][64 * PER] + sums[3][64 * PER]);
+  const bool none = l == 0.f;
+  if (tid < how.head_dim) put_float(none ? 0.f : ((sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid])) / l, const_cast<T*>(row_at<T>(a.out, b, i, h)) + tid);
+  if (tid == 0) a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------------------------ backward: dq, the rows' statistics, and the bias gradient's sums by relative position
@@ -673,6 +833,9 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
         const f32x16 s = rows_product<T, DH>(K, kl, q, l32, half);
         if (careful) load_own<T, DH>(d, row_at<T>(a.dout, b, qi, h), half, how.head_dim, valid);
         const f32x16 dp = rows_product<T, DH>(V, kl, d, l32, half);
+        Columns<T, DH> cols;
+        constexpr bool early = DH * sizeof(T) != 256;          // heads of 128 in bf16 have no registers for them meanwhile
+        if (early && !careful) load_columns<T, DH>(cols, K, kl, lane);
         const bool whole = k0 + 31 < sq.n_k && q0 + 31 < sq.n_q && (!causal || k0 + 31 <= pos0);
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;
         const int first = near ? k0 - pos + reach + kBiasPad + 4 * half : 0;
@@ -724,7 +887,10 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
           else above += sum;
         }
         if (careful && !whole) columns_exactly<T, DH>(dq, K, kl, ds, seen, lane);
-        else columns_product<T, DH>(dq, K, kl, t, lane);
+        else {
+          if (careful || !early) load_columns<T, DH>(cols, K, kl, lane);
+          columns_product<T, DH>(dq, cols, t);
+        }
       }
     }
     transfers_upto<0>();
@@ -858,6 +1024,8 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
         const f32x16 s = rows_product<T, DH>(Q, ql, k, l32, half);
         if (careful) load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
         const f32x16 dp = rows_product<T, DH>(D, ql, vv, l32, half);
+        Columns<T, DH> cols;
+        if (!careful) load_columns<T, DH>(cols, D, ql, lane);
         const bool whole = k0 + 31 < sq.n_k && q0 + 31 < sq.n_q && (!causal || k0 + 31 <= pos0);
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;
         float p[16], ds[16];
@@ -897,8 +1065,10 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
           columns_exactly<T, DH>(dv, D, ql, p, seen, lane);
           columns_exactly<T, DH>(dk, Q, ql, ds, seen, lane);
         } else {
-          columns_product<T, DH>(dv, D, ql, tp, lane);
-          columns_product<T, DH>(dk, Q, ql, td, lane);
+          if (careful) load_columns<T, DH>(cols, D, ql, lane);
+          columns_product<T, DH>(dv, cols, tp);
+          load_columns<T, DH>(cols, Q, ql, lane);
+          columns_product<T, DH>(dk, cols, td);
         }
       }
     }
@@ -957,39 +1127,46 @@ template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), i
 constexpr int kForwardWaves = 4, kQueryWaves = 4, kKeyWaves = 4;
 int64_t blocks_of(int n, int block, int heads, int batch) { return (int64_t)((n + block - 1) / block) * heads * batch; }
 
+int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
+
 // Few queries: those of the heads that share a K/V head fit two waves' columns, or the blocks of the other kernel would leave most of the chip idle over many keys.
 bool few_queries(const zgr_attention& how) {
   const int64_t rows = (int64_t)(how.n_head / how.n_kv_head) * how.n_q;
-  return rows <= 64 || (blocks_of(how.n_q, 32 * kForwardWaves, how.n_head, how.batch) <= 128 && how.n_k >= 1024);
+  return how.n_k > 0 && (rows <= 64 || (blocks_of(how.n_q, 32 * kForwardWaves, how.n_head, how.batch) <= 128 && how.n_k >= 1024));
 }
-// Chunks: some 2048 blocks in all, of 64 keys at least (a tile for each wave).
-struct Chunks { int keys, splits; int64_t blocks; };
-Chunks chunks_of(const zgr_attention& how) {
-  const int64_t items = ((int64_t)(how.n_head / how.n_kv_head) * how.n_q + 31) / 32 * how.n_kv_head * how.batch;
-  int64_t keys = ((int64_t)how.n_k * items + 2047) / 2048;
-  keys = (keys + 63) / 64 * 64;
-  if (keys < 64) keys = 64;
-  Chunks c;
-  c.keys = (int)keys;
-  c.splits = how.n_k ? (int)((how.n_k + keys - 1) / keys) : 1;
-  c.blocks = items * c.splits;
-  return c;
+FewWork few_work(const zgr_attention& how, bool& even) {
+  FewWork w;
+  const int64_t rows = (int64_t)(how.n_head / how.n_kv_head) * how.n_q;
+  w.row_blocks = (int)((rows + 31) / 32);
+  w.rows = (int)(rows < 32 ? rows : 32);
+  const int64_t items = (int64_t)w.row_blocks * how.n_kv_head * how.batch;
+  even = how.batch <= kFewBatch && how.n_k > 32;
+  const int resident = how.dtype == ZGR_F32 && how.head_dim > 64 ? 2 : 4;      // waves of a CU, by LDS and registers
+  w.workers = (int)(even ? resident * 256 : items);
+  return w;
 }
-size_t part_bytes(const zgr_attention& how, int dh) {
+template <typename T, int DH> size_t part_bytes(const zgr_attention& how) {
+  bool even;
+  const FewWork w = few_work(how, even);
+  return even ? (size_t)w.workers * 2 * w.rows * (DH + 2) * 4 : 0;
+}
+size_t few_bytes(const zgr_attention& how) {
   if (!few_queries(how)) return 0;
-  const Chunks c = chunks_of(how);
-  return c.splits == 1 ? 0 : ((size_t)c.splits * how.batch * how.n_head * how.n_q * (dh + 2) * 4 + 255) / 256 * 256;
+  const int d = padded_dim(how.head_dim);
+  const size_t part = d == 32 ? part_bytes<float, 32>(how) : d == 64 ? part_bytes<float, 64>(how) : part_bytes<float, 128>(how);
+  return part ? (part + 255) / 256 * 256 + ((size_t)how.batch + 1) * 8 : 0;
 }
 
 template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStream_t s) {
   if (!few_queries(a.how))
     return start(heads_forward_kernel<T, DH, kForwardWaves>, (blocks_of(a.how.n_q, 32 * kForwardWaves, a.how.n_head, a.how.batch) + 7) / 8 * 8, 64 * kForwardWaves, forward_lds<T, DH>(a.how), s, a);
-  const Chunks c = chunks_of(a.how);
+  bool even;
+  const FewWork w = few_work(a.how, even);
   float* part = reinterpret_cast<float*>(a.workspace);
-  hipError_t e = start(heads_few_kernel<T, DH>, c.blocks, 64 * kFewWaves, FewShape<T, DH>::lds, s, a, c.keys, c.splits, part);
-  if (e != hipSuccess || c.splits == 1) return e;
-  const int64_t rows = (int64_t)a.how.batch * a.how.n_head * a.how.n_q;
-  return start(heads_join_kernel<T, DH>, (rows + 3) / 4, 256, 0, s, a, c.splits, (const float*)part);
+  int64_t* ahead = reinterpret_cast<int64_t*>(a.workspace + (part_bytes<T, DH>(a.how) + 255) / 256 * 256);
+  hipError_t e = start(heads_few_kernel<T, DH>, w.workers, 64, FewShape<T, DH>::ring * FewShape<T, DH>::tile, s, a, w, even ? 1 : 0, part, ahead);
+  if (e != hipSuccess || !even) return e;
+  return start(heads_join_kernel<T, DH>, (int64_t)a.how.batch * a.how.n_head * a.how.n_q, 256, 0, s, a, w, (const float*)part, (const int64_t*)ahead);
 }
 
 size_t stats_bytes(const zgr_attention& how) { return ((size_t)how.batch * how.n_head * 2 * (size_t)stat_rows(how.n_q) * 4 + 255) / 256 * 256; }
@@ -1005,11 +1182,11 @@ template <typename T, int DH> hipError_t backward(const AttentionArgs& a, hipStr
   return hipGetLastError();
 }
 
-int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
+
 
 }  // namespace
 
-size_t attention_workspace(const zgr_attention& how) { return part_bytes(how, padded_dim(how.head_dim)); }
+size_t attention_workspace(const zgr_attention& how) { return few_bytes(how); }
 size_t attention_backward_workspace(const zgr_attention& how) {
   return stats_bytes(how) + (how.bias ? ((size_t)parts_of(how) * how.n_head * (2 * (size_t)how.bias_reach + 1) * 4 + 255) / 256 * 256 : 0);
 }
