@@ -283,11 +283,27 @@ template <typename T> __device__ __forceinline__ void stage_bias(float* lds, con
 __host__ __device__ inline int bias_places(const zgr_attention& h) { return h.bias ? 2 * h.bias_reach + 1 + 2 * kBiasPad : 0; }
 __host__ __device__ inline int bias_bytes(const zgr_attention& h) { return (bias_places(h) * 4 + 15) / 16 * 16; }
 
-// Consecutive block ids go round-robin to the 8 XCDs; every XCD gets an equal run of the work, so that the blocks of a head share one L2.
-__device__ __forceinline__ int64_t place_of_block(int64_t total) {
+// What a block works on: `rank` counts the blocks of a head from the one with the most work (under the causal mask) to the one with the least, `part` the heads that share a unit's K and
+// V (or the slices of its work).  Consecutive block ids go round-robin to the 8 XCDs, each with an L2 of its own.  by_unit: each unit belongs to an XCD, and the blocks with the most work of
+// all its units go first, so that the short ones fill the gaps at the end; where that would leave XCDs with more units than others, every XCD gets an equal run of blocks, unit by unit.
+struct Grid { int units, parts, ranks, by_unit; };
+__host__ __device__ inline int64_t blocks_of(const Grid& g) {
+  return g.by_unit ? (int64_t)8 * ((g.units + 7) / 8) * g.parts * g.ranks : ((int64_t)g.units * g.parts * g.ranks + 7) / 8 * 8;
+}
+struct Place { int unit, part, rank; };
+__device__ __forceinline__ bool place_of_block(const Grid& g, Place& p) {
   const int xcd = blockIdx.x & 7;
-  const int64_t local = blockIdx.x >> 3, q = total >> 3, rem = total & 7;
-  return local >= q + (xcd < rem ? 1 : 0) ? -1 : xcd * q + (xcd < rem ? xcd : rem) + local;
+  const uint32_t local = blockIdx.x >> 3;
+  if (g.by_unit) {
+    const uint32_t most = (uint32_t)(g.units + 7) / 8, j = local % most, rest = local / most;
+    p.unit = xcd + 8 * (int)j, p.part = (int)(rest % (uint32_t)g.parts), p.rank = (int)(rest / (uint32_t)g.parts);
+    return p.unit < g.units;
+  }
+  const uint32_t each = (uint32_t)g.parts * (uint32_t)g.ranks, total = (uint32_t)g.units * each, q = total >> 3, rem = total & 7;
+  if (local >= q + ((uint32_t)xcd < rem ? 1 : 0)) return false;
+  const uint32_t at = (uint32_t)xcd * q + ((uint32_t)xcd < rem ? (uint32_t)xcd : rem) + local, rest = at % each;
+  p.unit = (int)(at / each), p.rank = (int)(rest / (uint32_t)g.parts), p.part = (int)(rest % (uint32_t)g.parts);
+  return true;
 }
 
 template <typename T> __device__ __forceinline__ const T* row_at(const zgr_heads& x, int b, int64_t t, int h) { return (const T*)x.data + b * x.batch + t * x.token + h * x.head; }
@@ -348,16 +364,15 @@ template <int DH> __device__ __forceinline__ void raise_maximum(float top, float
 
 // ------------------------------------------------------------------------------------------------ forward
 template <typename T, int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs a, Grid grid) {
   using Sh = Shape<T, DH>;
   constexpr int QB = 32 * NW, KB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);      // PER: transfers of a wave for a stage
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int qblocks = (how.n_q + QB - 1) / QB;
-  const int64_t place = place_of_block((int64_t)qblocks * how.n_head * how.batch);
-  if (place < 0) return;
-  const int64_t bh = place / qblocks;
-  const int qb = qblocks - 1 - (int)(place - bh * qblocks), b = (int)(bh / how.n_head), h = (int)(bh - (int64_t)b * how.n_head), hk = h / (how.n_head / how.n_kv_head);
+  [[maybe_unused]] const int qblocks = grid.ranks;
+  Place place;
+  if (!place_of_block(grid, place)) return;
+  const int qb = qblocks - 1 - place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head, h = hk * grid.parts + place.part;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
   float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
@@ -765,16 +780,15 @@ __global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, FewWor
 // ------------------------------------------------------------------------------------------------ backward: dq, the rows' statistics, and the bias gradient's sums by relative position
 // stats: [batch][head][2][stat_rows]: log2 of each row's sum of exponentials, +infinity for a row that has no probabilities, and do . o.
 template <typename T, int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_dq_kernel(AttentionArgs a, float* __restrict__ stats, float* __restrict__ parts) {
+__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_dq_kernel(AttentionArgs a, float* __restrict__ stats, float* __restrict__ parts, Grid grid) {
   using Sh = Shape<T, DH>;
   constexpr int QB = 32 * NW, KB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int qblocks = (how.n_q + QB - 1) / QB;
-  const int64_t place = place_of_block((int64_t)qblocks * how.n_head * how.batch);
-  if (place < 0) return;
-  const int64_t bh = place / qblocks;
-  const int qb = qblocks - 1 - (int)(place - bh * qblocks), b = (int)(bh / how.n_head), h = (int)(bh - (int64_t)b * how.n_head), hk = h / (how.n_head / how.n_kv_head);
+  [[maybe_unused]] const int qblocks = grid.ranks;
+  Place place;
+  if (!place_of_block(grid, place)) return;
+  const int qb = qblocks - 1 - place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head, h = hk * grid.parts + place.part;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
   float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
@@ -946,16 +960,15 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
 
 // ------------------------------------------------------------------------------------------------ backward: dk, dv
 template <typename T, int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ stats) {
+__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ stats, Grid grid, float* __restrict__ part) {
   using Sh = Shape<T, DH>;
   constexpr int KB = 32 * NW, QB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
-  const int kblocks = (how.n_k + KB - 1) / KB, group = how.n_head / how.n_kv_head;
-  const int64_t place = place_of_block((int64_t)kblocks * how.n_kv_head * how.batch);
-  if (place < 0) return;
-  const int64_t bh = place / kblocks;
-  const int kb = (int)(place - bh * kblocks), b = (int)(bh / how.n_kv_head), hk = (int)(bh - (int64_t)b * how.n_kv_head);
+  const int group = how.n_head / how.n_kv_head;
+  Place place;
+  if (!place_of_block(grid, place)) return;
+  const int kb = place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
   float* rows_stats = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);      // [ring][2][64]
@@ -969,7 +982,10 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
   if (block_k0 >= sq.n_k) qbegin = sq.n_q;
   if (k0 >= sq.n_k) wave_qbegin = sq.n_q;
   qbegin = qbegin / QB * QB;
-  const int per_head = sq.n_q > qbegin ? (sq.n_q - qbegin + QB - 1) / QB : 0, stages = per_head * group;
+  const int per_head = sq.n_q > qbegin ? (sq.n_q - qbegin + QB - 1) / QB : 0, all_stages = per_head * group;
+  // this block's slice of them
+  const int slice = (int)((int64_t)all_stages * place.part / grid.parts), stages = (int)((int64_t)all_stages * (place.part + 1) / grid.parts) - slice;
+  const int first_head = per_head ? slice / per_head : 0, first_query = qbegin + (per_head ? slice - first_head * per_head : 0) * QB;
   const int64_t n_stats = stat_rows(how.n_q);
   struct At { int st, h, first; };                          // a stage's number, head and first query
   auto stage = [&](const At& at) {
@@ -992,7 +1008,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
   f32x16 dk[DH / 32], dv[DH / 32];
   auto pass = [&](auto again) -> bool {                     // whether a row's result is not finite; again: then once more, with hidden pairs left out of the products (columns_exactly)
     constexpr bool careful = decltype(again)::value;
-    At ahead{0, hk * group, qbegin};
+    At ahead{0, hk * group + first_head, first_query};
     if (stages)
 #pragma unroll
       for (int i = 0; i < Sh::ring - 1; ++i) { stage(ahead); next(ahead); }
@@ -1002,9 +1018,9 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
     }
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) dk[f] = dv[f] = zeros16();
-    At here{0, hk * group, qbegin};
+    At here{0, hk * group + first_head, first_query};
     for (int st = 0; st < stages; ++st, next(here)) {
-      if (here.first == qbegin && biased) {                 // another head
+      if ((st == 0 || here.first == qbegin) && biased) {    // another head
         if (st) block_barrier();
         stage_bias<T>(by_delta, how, here.h);
       }
@@ -1086,8 +1102,31 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
   if (!valid)
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) dk[f] = dv[f] = zeros16();
+  if (grid.parts > 1) {                                     // [2][slices][units][n_k][head_dim], for heads_slices_kernel
+    const int64_t rows = (int64_t)grid.units * how.n_k, row = (int64_t)place.unit * how.n_k + kj;
+    store_columns<float, DH>(part + (place.part * rows + row) * how.head_dim, dk, how.scale, half, how.head_dim);
+    store_columns<float, DH>(part + ((grid.parts + place.part) * rows + row) * how.head_dim, dv, 1.0f, half, how.head_dim);
+    return;
+  }
   store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dk, b, kj, hk)), dk, how.scale, half, how.head_dim);
   store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dv, b, kj, hk)), dv, 1.0f, half, how.head_dim);
+}
+
+// dk and dv from their slices' sums, in the slices' order: four entries a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) heads_slices_kernel(AttentionArgs a, const float* __restrict__ part, int slices) {
+  const zgr_attention& how = a.how;
+  const int quads = how.head_dim / 4;
+  const int64_t rows = (int64_t)how.batch * how.n_kv_head * how.n_k, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= rows * quads) return;
+  const int64_t row = at / quads, unit = row / how.n_k;
+  const int c = (int)(at - row * quads) * 4, key = (int)(row - unit * how.n_k), b = (int)(unit / how.n_kv_head), hk = (int)(unit - (int64_t)b * how.n_kv_head);
+  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(part + (blockIdx.y * (int64_t)slices * rows + row) * how.head_dim + c);
+  f32x4_t v = *p;
+#pragma unroll 4
+  for (int s = 1; s < slices; ++s) v += p[s * rows * quads];
+  const float x[4] = {v[0], v[1], v[2], v[3]};
+  store_run(const_cast<T*>(row_at<T>(blockIdx.y ? a.dv : a.dk, b, key, hk)) + c, x);
 }
 
 // ------------------------------------------------------------------------------------------------ dbias: the parts' sums by relative position, then by bucket
@@ -1117,7 +1156,7 @@ template <typename T, int DH, int NW> int dq_lds(const zgr_attention& how) { ret
 template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + Shape<T, DH>::ring * 128 * 4 + bias_bytes(how); }
 
 template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), int64_t blocks, int threads, int lds, hipStream_t s, A... args) {
-  if (!blocks) return hipSuccess;
+  if (!blocks) return hipSuccess;                           // nothing of its kind
   if (lds > 65536)
     if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds); e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, s, args...);
@@ -1125,14 +1164,32 @@ template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), i
 }
 
 constexpr int kForwardWaves = 4, kQueryWaves = 4, kKeyWaves = 4;
-int64_t blocks_of(int n, int block, int heads, int batch) { return (int64_t)((n + block - 1) / block) * heads * batch; }
+// Blocks of n rows, `parts` for each unit (a K/V head of a sequence).
+Grid grid_of(const zgr_attention& how, int n, int block, int parts) {
+  Grid g;
+  g.units = how.batch * how.n_kv_head, g.parts = parts, g.ranks = (n + block - 1) / block;
+  g.by_unit = (g.units + 7) / 8 * 8 <= g.units + g.units / 8;
+  return g;
+}
+Grid query_grid(const zgr_attention& how, int waves) { return grid_of(how, how.n_q, 32 * waves, how.n_head / how.n_kv_head); }
+// Keys: a block walks the queries of every head of its unit.  Where that makes few blocks, whose longest would be waited for, they are cut into slices of equal length, up to some 512 blocks
+// in all: slices cost a write and a read of dk and dv in fp32 each.  2 x 2047 tokens, 32 heads of 128 on 8, backward: 626 us without, 447 cut in two, 477 in three; 4096 tokens, 16 heads of 64 on
+// 4: 682, 287 (four slices), 286 (eight); where 512 blocks are there already, a second slice took 144 us to 198.
+Grid key_grid(const zgr_attention& how) {
+  Grid g = grid_of(how, how.n_k, 32 * kKeyWaves, 1);
+  const int64_t blocks = (int64_t)g.units * g.ranks, walk = (int64_t)((how.n_q + 63) / 64) * (how.n_head / how.n_kv_head);
+  int slices = blocks ? (int)((512 + blocks - 1) / blocks) : 1;
+  if (slices > walk / 4) slices = (int)(walk / 4);
+  g.parts = slices < 1 ? 1 : slices;
+  return g;
+}
 
 int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
 
 // Few queries: those of the heads that share a K/V head fit two waves' columns, or the blocks of the other kernel would leave most of the chip idle over many keys.
 bool few_queries(const zgr_attention& how) {
   const int64_t rows = (int64_t)(how.n_head / how.n_kv_head) * how.n_q;
-  return how.n_k > 0 && (rows <= 64 || (blocks_of(how.n_q, 32 * kForwardWaves, how.n_head, how.batch) <= 128 && how.n_k >= 1024));
+  return how.n_k > 0 && (rows <= 64 || ((int64_t)((how.n_q + 32 * kForwardWaves - 1) / (32 * kForwardWaves)) * how.n_head * how.batch <= 128 && how.n_k >= 1024));
 }
 FewWork few_work(const zgr_attention& how, bool& even) {
   FewWork w;
@@ -1158,8 +1215,10 @@ size_t few_bytes(const zgr_attention& how) {
 }
 
 template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStream_t s) {
-  if (!few_queries(a.how))
-    return start(heads_forward_kernel<T, DH, kForwardWaves>, (blocks_of(a.how.n_q, 32 * kForwardWaves, a.how.n_head, a.how.batch) + 7) / 8 * 8, 64 * kForwardWaves, forward_lds<T, DH>(a.how), s, a);
+  if (!few_queries(a.how)) {
+    const Grid g = query_grid(a.how, kForwardWaves);
+    return start(heads_forward_kernel<T, DH, kForwardWaves>, blocks_of(g), 64 * kForwardWaves, forward_lds<T, DH>(a.how), s, a, g);
+  }
   bool even;
   const FewWork w = few_work(a.how, even);
   float* part = reinterpret_cast<float*>(a.workspace);
@@ -1172,24 +1231,33 @@ template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStre
 size_t stats_bytes(const zgr_attention& how) { return ((size_t)how.batch * how.n_head * 2 * (size_t)stat_rows(how.n_q) * 4 + 255) / 256 * 256; }
 int parts_of(const zgr_attention& how) { return how.batch * ((how.n_q + 32 * kQueryWaves - 1) / (32 * kQueryWaves)); }
 
+size_t parts_bytes(const zgr_attention& how) { return how.bias ? ((size_t)parts_of(how) * how.n_head * (2 * (size_t)how.bias_reach + 1) * 4 + 255) / 256 * 256 : 0; }
+size_t slices_bytes(const zgr_attention& how) {
+  const Grid g = key_grid(how);
+  return g.parts > 1 ? (size_t)2 * g.parts * g.units * how.n_k * how.head_dim * 4 : 0;
+}
+
 template <typename T, int DH> hipError_t backward(const AttentionArgs& a, hipStream_t s) {
   float* stats = reinterpret_cast<float*>(a.workspace);
   float* parts = a.dbias ? reinterpret_cast<float*>(a.workspace + stats_bytes(a.how)) : nullptr;
-  hipError_t e = start(heads_dq_kernel<T, DH, kQueryWaves>, (blocks_of(a.how.n_q, 32 * kQueryWaves, a.how.n_head, a.how.batch) + 7) / 8 * 8, 64 * kQueryWaves, dq_lds<T, DH, kQueryWaves>(a.how), s, a, stats, parts);
-  if (e == hipSuccess) e = start(heads_dkv_kernel<T, DH, kKeyWaves>, (blocks_of(a.how.n_k, 32 * kKeyWaves, a.how.n_kv_head, a.how.batch) + 7) / 8 * 8, 64 * kKeyWaves, dkv_lds<T, DH>(a.how), s, a, stats);
+  float* slices = reinterpret_cast<float*>(a.workspace + stats_bytes(a.how) + parts_bytes(a.how));
+  const Grid gq = query_grid(a.how, kQueryWaves), gk = key_grid(a.how);
+  hipError_t e = start(heads_dq_kernel<T, DH, kQueryWaves>, blocks_of(gq), 64 * kQueryWaves, dq_lds<T, DH, kQueryWaves>(a.how), s, a, stats, parts, gq);
+  if (e == hipSuccess) e = start(heads_dkv_kernel<T, DH, kKeyWaves>, blocks_of(gk), 64 * kKeyWaves, dkv_lds<T, DH>(a.how), s, a, (const float*)stats, gk, slices);
+  if (e == hipSuccess && gk.parts > 1) {
+    const int64_t quads = (int64_t)gk.units * a.how.n_k * (a.how.head_dim / 4);
+    hipLaunchKernelGGL((heads_slices_kernel<T>), dim3((unsigned)((quads + 255) / 256), 2), dim3(256), 0, s, a, slices, gk.parts);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || !parts) return e;
   hipLaunchKernelGGL((heads_dbias_kernel<T>), dim3(a.how.n_head), dim3(1024), (2 * a.how.bias_reach + 1) * 4, s, a.how, parts, parts_of(a.how), (T*)a.dbias);
   return hipGetLastError();
 }
 
-
-
 }  // namespace
 
 size_t attention_workspace(const zgr_attention& how) { return few_bytes(how); }
-size_t attention_backward_workspace(const zgr_attention& how) {
-  return stats_bytes(how) + (how.bias ? ((size_t)parts_of(how) * how.n_head * (2 * (size_t)how.bias_reach + 1) * 4 + 255) / 256 * 256 : 0);
-}
+size_t attention_backward_workspace(const zgr_attention& how) { return stats_bytes(how) + parts_bytes(how) + slices_bytes(how); }
 
 hipError_t launch_heads_forward(const AttentionArgs& a, hipStream_t s) {
   switch (padded_dim(a.how.head_dim) + a.how.dtype) {

@@ -91,7 +91,7 @@ zgr_status check_attention(const zgr_attention* h) {
     if (off(h->bias, bytes_of(h->dtype)) || off(h->bias_map, 4)) return refuse(ZGR_ERR_SHAPE, "bias or bias_map is not aligned");
   }
   if (off(h->q_lengths, 4) || off(h->k_lengths, 4) || off(h->q_start, 4)) return refuse(ZGR_ERR_SHAPE, "lengths and starts must lie on 4 bytes");
-  const int64_t blocks = (int64_t)(((h->n_q > h->n_k ? h->n_q : h->n_k) + 31) / 32) * h->n_head;
+  const int64_t blocks = (int64_t)(((h->n_q > h->n_k ? h->n_q : h->n_k) + 32) / 32) * h->n_head;
   if (h->batch && blocks > (kMostThreads >> 9) / h->batch) return refuse(ZGR_ERR_SHAPE, "too many blocks for one launch");
   return ZGR_OK;
 }
