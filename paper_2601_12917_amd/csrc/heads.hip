@@ -328,7 +328,7 @@ template <typename T, int DH> __device__ __forceinline__ void store_columns(T* r
 // use, the one whose readers may not have finished, and the ones between that are on their way.
 template <typename T, int DH> struct Shape {
   static constexpr int row = DH * (int)sizeof(T);
-  static constexpr int rows = row >= 256 ? 32 : 64, ring = row >= 512 ? 2 : 4;
+  static constexpr int rows = row >= 256 ? 32 : 64, ring = 2;
   static constexpr int bytes = rows * row;                  // of one operand's stage
 };
 template <int N> __device__ __forceinline__ void transfers_upto() {      // all but the last N of this wave's transfers have landed
