@@ -12,6 +12,8 @@
 #include "sublayer.h"
 #include "wave.h"
 
+#include <cmath>
+
 #include <type_traits>
 
 namespace zgr {
@@ -494,7 +496,8 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
 // (Blocks of equal chunks of a sequence: 16 sequences of 1000 to 16384 tokens 195 us, in chunks of 1024 keys, of which the last of three rounds of blocks was a third full, and
 // more in smaller ones.)
 template <typename T, int DH> struct FewShape {
-  static constexpr int row = DH * (int)sizeof(T), tile = 2 * 32 * row, ring = tile <= 8192 ? 4 : 2, per = tile / 1024;
+  static constexpr int row = DH * (int)sizeof(T), tile = 2 * 32 * row, ring = tile <= 8192 ? 2 : 1, per = tile / 1024;
+  static constexpr int resident = tile > 16384 ? 4 : 8;     // waves of a CU, by LDS and registers
 };
 constexpr int kFewBatch = 1024;                             // sequences whose tiles a wave counts for itself
 __device__ __forceinline__ void reads_done() {              // this wave's reads of LDS have returned
@@ -515,7 +518,7 @@ struct FewWork { int workers, row_blocks, rows; };          // rows: of an item,
 // part: [workers][2][rows][DH] sums and then [workers][2][rows][2] maxima (log2) and sums of exponentials; ahead: [batch + 1], the tiles in front of each sequence.
 // even = 0: a worker is an item.
 template <typename T, int DH>
-__global__ void __launch_bounds__(64, DH * sizeof(T) >= 256 ? 1 : 2) heads_few_kernel(AttentionArgs a, FewWork w, int even, float* __restrict__ part, int64_t* __restrict__ ahead) {
+__global__ void __launch_bounds__(64, DH * sizeof(T) >= 512 ? 1 : 2) heads_few_kernel(AttentionArgs a, FewWork w, int even, float* __restrict__ part, uint32_t* __restrict__ ahead) {
   using Sh = FewShape<T, DH>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
@@ -525,41 +528,41 @@ __global__ void __launch_bounds__(64, DH * sizeof(T) >= 256 ? 1 : 2) heads_few_k
   Cursor here{0, 0, 0, 0};
   int count;
   if (even) {
-    // the tiles of all sequences, and the place of this worker's first
-    int64_t total = 0;
-    for (int b0 = 0; b0 < how.batch; b0 += 64) {
+    // the tiles of all sequences, and the place of this worker's first; sequences of the 64 lanes at a time
+    uint32_t total = 0, lane_tiles = 0, lane_ahead = 0;
+    auto count_64 = [&](int b0, uint32_t before) {          // lane_ahead: the tiles in front of the lane's sequence; returns those up to the last lane's
       const int b = b0 + lane;
-      int64_t n = b < how.batch ? (int64_t)tiles_of(how, sequence_of(how, b)) * items : 0;
+      lane_tiles = b < how.batch ? (uint32_t)tiles_of(how, sequence_of(how, b)) : 0;
+      uint32_t upto = lane_tiles * (uint32_t)items;
 #pragma unroll
-      for (int o = 1; o < 64; o *= 2) n += __shfl_xor(n, o, 64);
-      total += n;
-    }
-    const int64_t workers = min((int64_t)w.workers, total);      // every one of them has a tile
-    if (blockIdx.x >= workers) return;
-    const int64_t from = first_tile(blockIdx.x, workers, total);
-    count = uniform_of((int)(first_tile(blockIdx.x + 1, workers, total) - from));
-    int64_t before = 0;
-    bool found = false;
+      for (int o = 1; o < 64; o *= 2) { const uint32_t v = (uint32_t)__shfl_up((int)upto, o, 64); if (lane >= o) upto += v; }
+      lane_ahead = before + upto - lane_tiles * (uint32_t)items;
+      return before + (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    };
     for (int b0 = 0; b0 < how.batch; b0 += 64) {
-      const int b = b0 + lane, tiles = b < how.batch ? tiles_of(how, sequence_of(how, b)) : 0;
-      const int64_t own = (int64_t)tiles * items;
-      int64_t upto = own;                                   // and those of the lanes below
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) { const int64_t v = __shfl_up(upto, o, 64); if (lane >= o) upto += v; }
-      if (blockIdx.x == 0 && b < how.batch) ahead[b] = before + upto - own;
-      const uint64_t beyond = __builtin_amdgcn_ballot_w64(b < how.batch && before + upto > from);
-      if (!found && beyond) {
-        const int at = __builtin_ctzll(beyond);
-        here.b = b0 + at;
-        here.tiles = __shfl(tiles, at, 64);
-        const int64_t in = from - (before + __shfl(upto - own, at, 64));
-        here.item = (int)(in / here.tiles), here.tile = (int)(in - (int64_t)here.item * here.tiles);
-        found = true;
-      }
-      before += __shfl(upto, 63, 64);
+      total = count_64(b0, total);
+      if (blockIdx.x == 0 && b0 + lane < how.batch) ahead[b0 + lane] = lane_ahead;
     }
     if (blockIdx.x == 0 && lane == 0) ahead[how.batch] = total;
-    here.b = uniform_of(here.b), here.item = uniform_of(here.item), here.tile = uniform_of(here.tile), here.tiles = uniform_of(here.tiles);
+    const int64_t workers = min((int64_t)w.workers, (int64_t)total);      // every one of them has a tile
+    if (blockIdx.x >= workers) return;
+    const uint32_t from = (uint32_t)first_tile(blockIdx.x, workers, total);
+    count = uniform_of((int)((uint32_t)first_tile(blockIdx.x + 1, workers, total) - from));
+    for (int b0 = (how.batch - 1) / 64 * 64; b0 >= 0; b0 -= 64) {      // the last sequence that doesn't begin behind it; with up to 64 of them they have just been counted
+      if (how.batch > 64) {
+        uint32_t before = 0;
+        for (int c = 0; c < b0; c += 64) before = count_64(c, before);
+        count_64(b0, before);
+      }
+      const uint64_t in_front = __builtin_amdgcn_ballot_w64(b0 + lane < how.batch && lane_ahead <= from);
+      if (in_front == 0) continue;
+      const int at = 63 - __builtin_clzll(in_front);
+      here.b = b0 + at;
+      here.tiles = __builtin_amdgcn_readlane((int)lane_tiles, at);
+      const uint32_t in = from - (uint32_t)__builtin_amdgcn_readlane((int)lane_ahead, at);
+      here.item = uniform_of((int)(in / (uint32_t)here.tiles)), here.tile = (int)(in - (uint32_t)here.item * (uint32_t)here.tiles);
+      break;
+    }
   } else {
     here.b = (int)(blockIdx.x / (unsigned)items), here.item = (int)(blockIdx.x % (unsigned)items);
     here.tiles = uniform_of(tiles_of(how, sequence_of(how, here.b)));
@@ -721,14 +724,14 @@ __global__ void __launch_bounds__(64, DH * sizeof(T) >= 256 ? 1 : 2) heads_few_k
 
 // The sums that several workers left of a row: a block each, every fourth worker to a wave.
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, FewWork w, const float* __restrict__ part, const int64_t* __restrict__ ahead) {
+__global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, FewWork w, const float* __restrict__ part, const uint32_t* __restrict__ ahead) {
   constexpr int PER = DH / 64 > 0 ? DH / 64 : 1;
   __shared__ float tops[4], sums[4][64 * PER + 1];
   const zgr_attention& how = a.how;
   const int64_t row = blockIdx.x;
   const int b = (int)(row / ((int64_t)how.n_head * how.n_q)), h = (int)(row / how.n_q % how.n_head), i = (int)(row % how.n_q), group = how.n_head / how.n_kv_head;
   const int r = (h % group) * how.n_q + i, items = w.row_blocks * how.n_kv_head;
-  const int64_t total = ahead[how.batch], tiles = (ahead[b + 1] - ahead[b]) / items, first = ahead[b] + ((int64_t)(h / group) * w.row_blocks + r / 32) * tiles;
+  const int64_t total = ahead[how.batch], tiles = (ahead[b + 1] - ahead[b]) / (uint32_t)items, first = ahead[b] + ((int64_t)(h / group) * w.row_blocks + r / 32) * tiles;
   const int64_t workers = min((int64_t)w.workers, total), g0 = ((first + 1) * workers - 1) / total, g1 = ((first + tiles) * workers - 1) / total;      // the workers of its first and last tile
   if (g0 == g1) return;                                     // which wrote it
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)(g1 - g0) + 1;
@@ -1186,20 +1189,27 @@ Grid key_grid(const zgr_attention& how) {
 
 int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
 
-// Few queries: those of the heads that share a K/V head fit two waves' columns, or the blocks of the other kernel would leave most of the chip idle over many keys.
+// Which of the two forward kernels: the sooner done by an estimate.  Blocks of queries walk all keys, 0.57 us (bf16, heads up to 64), 1.0 (128), 2.4 and 4.5 (fp32) a tile of 32, some
+// 768 blocks at a time.  Runs of tiles take 4 us for each 8 KiB tile of a worker's run, of which there are 2048 (1024), and 8 us more to begin with (the count, and the launch that joins
+// them).  Measured, blocks | runs: 1 query, 8 heads of 64, 1024 keys 23.7 | 14.1 us, 128 keys 7.7 | 13.8; 16 x 1 query, 32 heads of 128 on 8, 1024 keys 37.5 | 28.9, 256 keys 14.8 | 19.8;
+// 512 queries, 4 heads of 64, 4096 keys 85.6 | 39.0; 1500 queries on themselves, 8 heads 35.6 | 70.1; fp32, 16 x 16 queries, 8 heads of 64, 256 keys 25.4 | 22.8.
 bool few_queries(const zgr_attention& how) {
-  const int64_t rows = (int64_t)(how.n_head / how.n_kv_head) * how.n_q;
-  return how.n_k > 0 && (rows <= 64 || ((int64_t)((how.n_q + 32 * kForwardWaves - 1) / (32 * kForwardWaves)) * how.n_head * how.batch <= 128 && how.n_k >= 1024));
+  if (!how.n_k || !how.n_q || !how.batch) return false;
+  const int dim = padded_dim(how.head_dim), bytes = dim * (how.dtype == ZGR_F32 ? 4 : 2);
+  const double tiles = (how.n_k + 31) / 32, rows = (double)(how.n_head / how.n_kv_head) * how.n_q;
+  const double blocks = (double)((how.n_q + 32 * kForwardWaves - 1) / (32 * kForwardWaves)) * how.n_head * how.batch, tile_us = how.dtype == ZGR_F32 ? (dim > 64 ? 4.5 : 2.4) : (dim > 64 ? 1.0 : 0.57);
+  const double items = std::ceil(rows / 32) * how.n_kv_head * how.batch, workers = bytes > 256 ? 1024 : 2048;
+  return 8 + std::ceil(items * tiles / workers) * 4 * (bytes / 128.0) < tiles * tile_us * std::fmax(1.0, blocks / 768);
 }
+int few_resident(const zgr_attention& how) { return how.dtype == ZGR_F32 && how.head_dim > 64 ? FewShape<float, 128>::resident : FewShape<float, 64>::resident; }
 FewWork few_work(const zgr_attention& how, bool& even) {
   FewWork w;
   const int64_t rows = (int64_t)(how.n_head / how.n_kv_head) * how.n_q;
   w.row_blocks = (int)((rows + 31) / 32);
   w.rows = (int)(rows < 32 ? rows : 32);
   const int64_t items = (int64_t)w.row_blocks * how.n_kv_head * how.batch;
-  even = how.batch <= kFewBatch && how.n_k > 32;
-  const int resident = how.dtype == ZGR_F32 && how.head_dim > 64 ? 2 : 4;      // waves of a CU, by LDS and registers
-  w.workers = (int)(even ? resident * 256 : items);
+  even = how.batch <= kFewBatch && items * ((how.n_k + 31) / 32) < (int64_t)1 << 31;
+  w.workers = (int)(even ? few_resident(how) * 256 : items);
   return w;
 }
 template <typename T, int DH> size_t part_bytes(const zgr_attention& how) {
@@ -1211,7 +1221,7 @@ size_t few_bytes(const zgr_attention& how) {
   if (!few_queries(how)) return 0;
   const int d = padded_dim(how.head_dim);
   const size_t part = d == 32 ? part_bytes<float, 32>(how) : d == 64 ? part_bytes<float, 64>(how) : part_bytes<float, 128>(how);
-  return part ? (part + 255) / 256 * 256 + ((size_t)how.batch + 1) * 8 : 0;
+  return part ? (part + 255) / 256 * 256 + ((size_t)how.batch + 1) * 4 : 0;
 }
 
 template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStream_t s) {
@@ -1222,10 +1232,10 @@ template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStre
   bool even;
   const FewWork w = few_work(a.how, even);
   float* part = reinterpret_cast<float*>(a.workspace);
-  int64_t* ahead = reinterpret_cast<int64_t*>(a.workspace + (part_bytes<T, DH>(a.how) + 255) / 256 * 256);
+  uint32_t* ahead = reinterpret_cast<uint32_t*>(a.workspace + (part_bytes<T, DH>(a.how) + 255) / 256 * 256);
   hipError_t e = start(heads_few_kernel<T, DH>, w.workers, 64, FewShape<T, DH>::ring * FewShape<T, DH>::tile, s, a, w, even ? 1 : 0, part, ahead);
   if (e != hipSuccess || !even) return e;
-  return start(heads_join_kernel<T, DH>, (int64_t)a.how.batch * a.how.n_head * a.how.n_q, 256, 0, s, a, w, (const float*)part, (const int64_t*)ahead);
+  return start(heads_join_kernel<T, DH>, (int64_t)a.how.batch * a.how.n_head * a.how.n_q, 256, 0, s, a, w, (const float*)part, (const uint32_t*)ahead);
 }
 
 size_t stats_bytes(const zgr_attention& how) { return ((size_t)how.batch * how.n_head * 2 * (size_t)stat_rows(how.n_q) * 4 + 255) / 256 * 256; }
