@@ -1,17 +1,19 @@
 // RMS norms of queries and keys for each head with the position rotation in the same pass, and the gradient of both.
 //   y = g x / sqrt(mean x^2 + eps);  pairs (a, b) of the first rot_dim entries -> (a cos - b sin, b cos + a sin)
 // backward: dy = the rotation back of dz, h = g dy, dx = r (h - x r^2 mean(h x)), dg = sum over rows and heads of dy x r  (r = 1 / sqrt(mean x^2 + eps))
-// A group of L lanes holds one head of one row, V entries a lane, so that the mean is log2 L exchanges within the wave and the other half of a pair is
-// in the same lane or one exchange away.  A lane takes the same place of kRotateHeads heads of one row: their loads are in flight together and the row's angles are
-// read once.  Bound by memory: 4 bytes an entry of bf16 forward, 6 backward.  r is taken again in the backward pass (it costs nothing under the loads).
+// A group of L lanes holds one head of one row, eight entries a lane in two runs of four: where pairs are halves apart, the runs are, so that a pair is always in one lane and only the
+// mean takes exchanges (log2 L).  A lane takes the same place of kRotateHeads or kBackHeads heads of one row: their loads are in flight together and the row's angles are read once.
+// Bound by memory: 4 bytes an entry of bf16 forward, 6 backward.  4096 rows of 64 heads of 64 in bf16 take 18 us (3.7 TB/s) and, with the sums of the gains, 29 back;
+// 16384 rows of 40 heads of 128 take 81 (4.2) and 126 (4.0), 32768 rows of 32 heads of 64 in fp32 96 (5.6) and 110.  r is taken again in the backward pass, which costs nothing under the loads.
 #include "sublayer.h"
 
 namespace zgr {
 
 namespace {
 
-constexpr int kRotateHeads = 4;          // heads of a lane at once
-constexpr int kRotateParts = 512;        // blocks of the backward pass, each with its own sums of the gains' gradients
+constexpr int kRotateHeads = 4;          // heads of a lane at once, forward
+constexpr int kBackHeads = 2;            // and backward, where twice as much is held for each and more waves hide the loads better (four heads took 36 us for 29, and 192 for 126)
+constexpr int kRotateParts = 1024;       // blocks of the backward pass, each with its own sums of the gains' gradients (512: 35 and 174 us for 29 and 126, 2048: 33 and 130)
 
 template <int L> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
@@ -19,112 +21,80 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-struct Place {                           // what of a row a lane works on
-  int part;                              // lane's place in its head
-  int c;                                 // its first entry
-  bool inside;                           // of the head
-  int rot_at;                            // its first pair, -1: not rotated
-  bool second;                           // holds the second members (halves)
-  int other;                             // lane with the other members of its pairs (halves)
-};
-
-template <int V, int L> __device__ __forceinline__ Place place_of(const zgr_rotation& how) {
+// A lane's eight entries: four from `first` on and four from `second` on.
+struct Place { int first, second; bool inside, turned; };
+__device__ __forceinline__ Place place_of(const zgr_rotation& how, int part) {
   Place p;
-  const int lane = threadIdx.x & 63;
-  p.part = lane % L;
-  p.c = p.part * V;
-  p.inside = p.c < how.head_dim;
-  p.rot_at = -1;
-  p.second = false;
-  p.other = lane;
-  if (p.c < how.rot_dim) {
-    if (how.interleaved) p.rot_at = p.c / 2;
-    else {
-      const int half = how.rot_dim / 2;
-      p.second = p.c >= half;
-      p.rot_at = p.second ? p.c - half : p.c;
-      p.other = lane + (p.second ? -half : half) / V;
-    }
-  }
+  p.inside = 8 * part < how.head_dim;
+  p.turned = 8 * part < how.rot_dim;
+  const bool halves = p.turned && !how.interleaved;
+  p.first = halves ? 4 * part : 8 * part;
+  p.second = halves ? how.rot_dim / 2 + 4 * part : 8 * part + 4;
   return p;
 }
-
-template <int V> struct Angles { float c[V], s[V]; };      // of the lane's entries (both members of a neighbouring pair have the same)
-
-template <int V> __device__ __forceinline__ Angles<V> angles_of(const zgr_rotation& how, const Place& p, int row) {
-  Angles<V> t;
+template <typename T> __device__ __forceinline__ void load_eight(const T* head, const Place& p, float (&x)[8]) {
+  float a[4], b[4];
+  load_run(head + p.first, a);
+  load_run(head + p.second, b);
 #pragma unroll
-  for (int i = 0; i < V; ++i) { t.c[i] = 1.f; t.s[i] = 0.f; }
-  if (p.rot_at < 0) return t;
+  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+}
+template <typename T> __device__ __forceinline__ void store_eight(T* head, const Place& p, const float (&x)[8]) {
+  const float a[4] = {x[0], x[1], x[2], x[3]}, b[4] = {x[4], x[5], x[6], x[7]};
+  store_run(head + p.first, a);
+  store_run(head + p.second, b);
+}
+
+// cos and sin of the lane's four pairs; the row is the same for the wave
+__device__ __forceinline__ void angles_of(const zgr_rotation& how, const Place& p, int part, int row, float (&t)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { t[2 * i] = 1.f; t[2 * i + 1] = 0.f; }
+  if (how.rot_dim == 0) return;
   const int at = how.positions[row];
   if (at < 0 || at >= how.n_positions) {                   // no such row of the table: the result says so
 #pragma unroll
-    for (int i = 0; i < V; ++i) t.c[i] = t.s[i] = __uint_as_float(0x7FC00000u);
-    return t;
-  }
-  const float* e = how.table + ((int64_t)at * (how.rot_dim / 2) + p.rot_at) * 2;
-  if (how.interleaved) {
-    float f[V];
-    load_run<float, V>(e, f);
-#pragma unroll
-    for (int i = 0; i < V; ++i) { t.c[i] = f[i & ~1]; t.s[i] = f[i | 1]; }
-  } else {
-    float f[2 * V];
-    load_run<float, 2 * V>(e, f);
-#pragma unroll
-    for (int i = 0; i < V; ++i) { t.c[i] = f[2 * i]; t.s[i] = f[2 * i + 1]; }
-  }
-  return t;
+    for (int i = 0; i < 8; ++i) t[i] = p.turned ? __uint_as_float(0x7FC00000u) : t[i];
+  } else if (p.turned) load_run<float, 8>(how.table + ((int64_t)at * (how.rot_dim / 2) + 4 * part) * 2, t);
 }
-
-// forward: sign = 1, back: sign = -1.  Every lane of the wave comes here.
-template <int V> __device__ __forceinline__ void turn(const zgr_rotation& how, const Place& p, const Angles<V>& t, float sign, float (&y)[V]) {
-  if (how.rot_dim == 0) return;
-  float o[V];
-  if (how.interleaved) {
+// forward: by = 1, back: by = -1
+__device__ __forceinline__ void turn(bool interleaved, const float (&t)[8], float by, float (&y)[8]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = y[i ^ 1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = __shfl(y[i], p.other, 64);
-  }
-  if (p.rot_at < 0) return;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const bool second = how.interleaved ? (i & 1) : p.second;
-    y[i] = __builtin_fmaf(y[i], t.c[i], (second ? sign : -sign) * (o[i] * t.s[i]));
+  for (int i = 0; i < 4; ++i) {
+    const float a = interleaved ? y[2 * i] : y[i], b = interleaved ? y[2 * i + 1] : y[4 + i], s = by * t[2 * i + 1];
+    const float u = __builtin_fmaf(a, t[2 * i], -(b * s)), v = __builtin_fmaf(b, t[2 * i], a * s);
+    if (interleaved) { y[2 * i] = u; y[2 * i + 1] = v; }
+    else { y[i] = u; y[4 + i] = v; }
   }
 }
 
-template <typename T, int V> __device__ __forceinline__ void gains_of(const void* gain, const Place& p, float (&g)[V]) {
+template <typename T> __device__ __forceinline__ void gains_of(const void* gain, const Place& p, float (&g)[8]) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) g[i] = 1.f;
-  if (gain && p.inside) load_run((const T*)gain + p.c, g);
+  for (int i = 0; i < 8; ++i) g[i] = 1.f;
+  if (gain && p.inside) load_eight((const T*)gain, p, g);
 }
 
-template <typename T> __device__ __forceinline__ T* at(const zgr_heads& x, int64_t row, int head, int c) { return (T*)x.data + row * x.token + (int64_t)head * x.head + c; }
+template <typename T> __device__ __forceinline__ T* head_at(const zgr_heads& x, int64_t row, int head) { return (T*)x.data + row * x.token + (int64_t)head * x.head; }
 
 // A wave takes kRotateHeads x 64 / L heads of a row.
-template <typename T, int V, int L>
+template <typename T, int L, bool PAIRS>
 __global__ void __launch_bounds__(256) norm_rotate_kernel(RotateArgs a, int chunks, int64_t items) {
   constexpr int per = 64 / L;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (item >= items) return;
   const int64_t row = item / chunks;
   const int lane = threadIdx.x & 63, heads = a.how.q_heads + a.how.k_heads, first = (int)(item - row * chunks) * (per * kRotateHeads) + lane / L;
-  const Place p = place_of<V, L>(a.how);
-  float x[kRotateHeads][V];
+  const Place p = place_of(a.how, lane % L);
+  float x[kRotateHeads][8], t[8], gq[8], gk[8];
 #pragma unroll
   for (int u = 0; u < kRotateHeads; ++u) {
     const int h = first + u * per;
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
-    if (h < heads && p.inside) load_run(h < a.how.q_heads ? at<T>(a.q, row, h, p.c) : at<T>(a.k, row, h - a.how.q_heads, p.c), x[u]);
+    for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
+    if (h < heads && p.inside) load_eight(h < a.how.q_heads ? head_at<T>(a.q, row, h) : head_at<T>(a.k, row, h - a.how.q_heads), p, x[u]);
   }
-  const Angles<V> t = angles_of<V>(a.how, p, (int)row);
-  float gq[V], gk[V];
-  gains_of<T, V>(a.how.q_gain, p, gq);
-  gains_of<T, V>(a.how.k_gain, p, gk);
+  angles_of(a.how, p, lane % L, (int)row, t);
+  gains_of<T>(a.how.q_gain, p, gq);
+  gains_of<T>(a.how.k_gain, p, gk);
   const float inv = 1.0f / (float)a.how.head_dim;
 #pragma unroll
   for (int u = 0; u < kRotateHeads; ++u) {
@@ -132,52 +102,52 @@ __global__ void __launch_bounds__(256) norm_rotate_kernel(RotateArgs a, int chun
     const bool is_q = h < a.how.q_heads;
     float ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) ss = __builtin_fmaf(x[u][i], x[u][i], ss);
+    for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(x[u][i], x[u][i], ss);
     ss = lanes_sum<L>(ss);
     const float r = (is_q ? a.how.q_gain : a.how.k_gain) ? 1.0f / sqrtf(ss * inv + a.how.eps) : 1.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[u][i] = x[u][i] * r * (is_q ? gq[i] : gk[i]);
-    turn<V>(a.how, p, t, 1.0f, x[u]);
-    if (h < heads && p.inside) store_run(is_q ? at<T>(a.q_out, row, h, p.c) : at<T>(a.k_out, row, h - a.how.q_heads, p.c), x[u]);
+    for (int i = 0; i < 8; ++i) x[u][i] = x[u][i] * r * (is_q ? gq[i] : gk[i]);
+    if (p.turned) turn(PAIRS, t, 1.0f, x[u]);
+    if (h < heads && p.inside) store_eight(is_q ? head_at<T>(a.q_out, row, h) : head_at<T>(a.k_out, row, h - a.how.q_heads), p, x[u]);
   }
 }
 
-template <typename T, int V, int L>
+template <typename T, int L, bool PAIRS>
 __global__ void __launch_bounds__(256) norm_rotate_backward_kernel(RotateArgs a, int chunks, int64_t items) {
   constexpr int per = 64 / L;
-  __shared__ float sums[4][2 * V * L];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, heads = a.how.q_heads + a.how.k_heads;
-  const Place p = place_of<V, L>(a.how);
-  float gq[V], gk[V], dgq[V], dgk[V];
-  gains_of<T, V>(a.how.q_gain, p, gq);
-  gains_of<T, V>(a.how.k_gain, p, gk);
+  __shared__ float sums[4][2][8 * L];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), heads = a.how.q_heads + a.how.k_heads;
+  const Place p = place_of(a.how, lane % L);
+  float gq[8], gk[8], dgq[8], dgk[8];
+  gains_of<T>(a.how.q_gain, p, gq);
+  gains_of<T>(a.how.k_gain, p, gk);
 #pragma unroll
-  for (int i = 0; i < V; ++i) dgq[i] = dgk[i] = 0.f;
+  for (int i = 0; i < 8; ++i) dgq[i] = dgk[i] = 0.f;
   const float inv = 1.0f / (float)a.how.head_dim;
   for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < items; item += (int64_t)gridDim.x * 4) {
     const int64_t row = item / chunks;
-    const int first = (int)(item - row * chunks) * (per * kRotateHeads) + lane / L;
-    float x[kRotateHeads][V], d[kRotateHeads][V];
+    const int first = (int)(item - row * chunks) * (per * kBackHeads) + lane / L;
+    float x[kBackHeads][8], d[kBackHeads][8], t[8];
 #pragma unroll
-    for (int u = 0; u < kRotateHeads; ++u) {
+    for (int u = 0; u < kBackHeads; ++u) {
       const int h = first + u * per;
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[u][i] = d[u][i] = 0.f;
+      for (int i = 0; i < 8; ++i) x[u][i] = d[u][i] = 0.f;
       if (h < heads && p.inside) {
-        load_run(h < a.how.q_heads ? at<T>(a.q_out, row, h, p.c) : at<T>(a.k_out, row, h - a.how.q_heads, p.c), d[u]);
-        load_run(h < a.how.q_heads ? at<T>(a.q, row, h, p.c) : at<T>(a.k, row, h - a.how.q_heads, p.c), x[u]);
+        load_eight(h < a.how.q_heads ? head_at<T>(a.q_out, row, h) : head_at<T>(a.k_out, row, h - a.how.q_heads), p, d[u]);
+        load_eight(h < a.how.q_heads ? head_at<T>(a.q, row, h) : head_at<T>(a.k, row, h - a.how.q_heads), p, x[u]);
       }
     }
-    const Angles<V> t = angles_of<V>(a.how, p, (int)row);
+    angles_of(a.how, p, lane % L, (int)row, t);
 #pragma unroll
-    for (int u = 0; u < kRotateHeads; ++u) {
+    for (int u = 0; u < kBackHeads; ++u) {
       const int h = first + u * per;
       const bool is_q = h < a.how.q_heads;
-      turn<V>(a.how, p, t, -1.0f, d[u]);
+      if (p.turned) turn(PAIRS, t, -1.0f, d[u]);
       if ((is_q ? a.how.q_gain : a.how.k_gain) != nullptr) {      // the same for the lanes of a group: exchanges stay within it
         float ss = 0.f, hx = 0.f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < 8; ++i) {
           ss = __builtin_fmaf(x[u][i], x[u][i], ss);
           hx = __builtin_fmaf(d[u][i] * (is_q ? gq[i] : gk[i]), x[u][i], hx);
         }
@@ -185,78 +155,77 @@ __global__ void __launch_bounds__(256) norm_rotate_backward_kernel(RotateArgs a,
         hx = lanes_sum<L>(hx);
         const float r = 1.0f / sqrtf(ss * inv + a.how.eps), back = r * r * (hx * inv);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < 8; ++i) {
           const float dg = h < heads ? d[u][i] * x[u][i] * r : 0.f;
           dgq[i] += is_q ? dg : 0.f;
           dgk[i] += is_q ? 0.f : dg;
           d[u][i] = r * (d[u][i] * (is_q ? gq[i] : gk[i]) - x[u][i] * back);
         }
       }
-      if (h < heads && p.inside) store_run(is_q ? at<T>(a.dq, row, h, p.c) : at<T>(a.dk, row, h - a.how.q_heads, p.c), d[u]);
+      if (h < heads && p.inside) store_eight(is_q ? head_at<T>(a.dq, row, h) : head_at<T>(a.dk, row, h - a.how.q_heads), p, d[u]);
     }
   }
   if (!a.part) return;
 #pragma unroll
-  for (int i = 0; i < V; ++i)
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
     for (int o = L; o < 64; o *= 2) {
       dgq[i] += __shfl_xor(dgq[i], o, 64);
       dgk[i] += __shfl_xor(dgk[i], o, 64);
     }
-  if (lane < L) {
+  if (lane < L && p.inside) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      sums[wave][p.c + i] = dgq[i];
-      sums[wave][V * L + p.c + i] = dgk[i];
+    for (int i = 0; i < 8; ++i) {
+      const int c = i < 4 ? p.first + i : p.second + i - 4;
+      sums[wave][0][c] = dgq[i];
+      sums[wave][1][c] = dgk[i];
     }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.how.head_dim; i += 256) {
-    const int c = i < a.how.head_dim ? i : V * L + i - a.how.head_dim;
-    a.part[(int64_t)blockIdx.x * 2 * a.how.head_dim + i] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+    const int k = i >= a.how.head_dim, c = i - k * a.how.head_dim;
+    a.part[(int64_t)blockIdx.x * 2 * a.how.head_dim + i] = (sums[0][k][c] + sums[1][k][c]) + (sums[2][k][c] + sums[3][k][c]);
   }
 }
 
-// Entries of a lane: 16 bytes, or 8 entries' half of that where the halves of the rotated part don't fall on runs of 8.
-int run_of(const zgr_rotation& how) { return how.dtype == ZGR_BF16 && (how.interleaved || how.rot_dim % 16 == 0) ? 8 : 4; }
 int lanes_of(const zgr_rotation& how) {
   int l = 1;
-  while (l * run_of(how) < how.head_dim) l *= 2;
+  while (8 * l < how.head_dim) l *= 2;
   return l;
 }
-int chunks_of(const zgr_rotation& how) {
-  const int per = 64 / lanes_of(how) * kRotateHeads;
+int chunks_of(const zgr_rotation& how, int each) {
+  const int per = 64 / lanes_of(how) * each;
   return (how.q_heads + how.k_heads + per - 1) / per;
 }
 
-template <typename T, int V, int L>
+template <typename T, int L, bool PAIRS>
 hipError_t start(const RotateArgs& a, bool backward, hipStream_t s) {
-  const int chunks = chunks_of(a.how);
+  const int chunks = chunks_of(a.how, backward ? kBackHeads : kRotateHeads);
   const int64_t items = (int64_t)a.how.rows * chunks;
-  if (backward) hipLaunchKernelGGL((norm_rotate_backward_kernel<T, V, L>), dim3(rotate_parts(a.how)), dim3(256), 0, s, a, chunks, items);
-  else hipLaunchKernelGGL((norm_rotate_kernel<T, V, L>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a, chunks, items);
+  if (backward) hipLaunchKernelGGL((norm_rotate_backward_kernel<T, L, PAIRS>), dim3(rotate_parts(a.how)), dim3(256), 0, s, a, chunks, items);
+  else hipLaunchKernelGGL((norm_rotate_kernel<T, L, PAIRS>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a, chunks, items);
   return hipGetLastError();
 }
-template <typename T, int V>
+template <typename T, bool PAIRS>
 hipError_t start_lanes(const RotateArgs& a, bool backward, hipStream_t s) {
   switch (lanes_of(a.how)) {
-    case 1: return start<T, V, 1>(a, backward, s);
-    case 2: return start<T, V, 2>(a, backward, s);
-    case 4: return start<T, V, 4>(a, backward, s);
-    case 8: return start<T, V, 8>(a, backward, s);
-    case 16: return start<T, V, 16>(a, backward, s);
-    case 32: return start<T, V, 32>(a, backward, s);
-    default: return start<T, V, 64>(a, backward, s);
+    case 1: return start<T, 1, PAIRS>(a, backward, s);
+    case 2: return start<T, 2, PAIRS>(a, backward, s);
+    case 4: return start<T, 4, PAIRS>(a, backward, s);
+    case 8: return start<T, 8, PAIRS>(a, backward, s);
+    case 16: return start<T, 16, PAIRS>(a, backward, s);
+    default: return start<T, 32, PAIRS>(a, backward, s);
   }
 }
 hipError_t start_any(const RotateArgs& a, bool backward, hipStream_t s) {
-  if (a.how.dtype == ZGR_F32) return start_lanes<float, 4>(a, backward, s);
-  return run_of(a.how) == 8 ? start_lanes<bf16_bits, 8>(a, backward, s) : start_lanes<bf16_bits, 4>(a, backward, s);
+  if (a.how.dtype == ZGR_F32) return a.how.interleaved ? start_lanes<float, true>(a, backward, s) : start_lanes<float, false>(a, backward, s);
+  return a.how.interleaved ? start_lanes<bf16_bits, true>(a, backward, s) : start_lanes<bf16_bits, false>(a, backward, s);
 }
 
 }  // namespace
 
 int rotate_parts(const zgr_rotation& how) {
-  const int64_t blocks = ((int64_t)how.rows * chunks_of(how) + 3) / 4;
+  const int64_t blocks = ((int64_t)how.rows * chunks_of(how, kBackHeads) + 3) / 4;
   return (int)(blocks < kRotateParts ? blocks : kRotateParts);
 }
 hipError_t launch_norm_rotate(const RotateArgs& a, hipStream_t s) { return start_any(a, false, s); }
