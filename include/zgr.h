@@ -318,7 +318,8 @@ zgr_status zgr_relative_buckets(int32_t buckets, int32_t reach, int32_t causal, 
 
 /* out_i = sum_j softmax_j(scale q_i . k_j + bias[map[clamp(j - (start + i), -reach, reach) + reach]][head]) v_j over the keys j that query i of its sequence sees:
  * j < k_lengths[b], and j <= q_start[b] + i with causal = 1, for i < q_lengths[b].  Query head h reads K/V head h / (n_head / n_kv_head).  A row that sees nothing, or lies
- * behind its length, gets zeros (lse -inf) and passes no gradient on.  What hidden places hold, NaN and infinities among it, changes nothing.          */
+ * behind its length, gets zeros (lse -inf) and passes no gradient on.  What hidden places hold, NaN and infinities among it, reaches no result (with such in a tile of keys that some rows see, those
+ * rows may be summed in another order: the last bits).                                                          */
 typedef struct {
   int32_t dtype, batch, n_q, n_k, n_head, n_kv_head;
   int32_t head_dim;                 /* a multiple of 8 up to 128                                      */

@@ -1,0 +1,188 @@
+"""An attention sublayer as a model has it, made of the operators in sublayer.py: trained through torch's autograd, and run token by token over a cache of keys and values.
+
+    x [batch, tokens, d], the residual stream
+    q, k, v = x W_qkv;  q, k normalised for each head and rotated by their positions;  attention with a bias by relative position
+    x + dropout(o W_out + b)
+
+The two projections are the caller's products (torch's); everything between and behind them is one launch or two each way.
+`python -m paper_2601_12917_amd.attention_block` trains one on a small synthetic task, answers a prompt with it token by token, and says how long both take.
+"""
+import argparse
+import json
+import time
+
+import torch
+
+from . import sublayer as S
+
+
+class _NormRotate(torch.autograd.Function):
+    """x [tokens, (heads + 2 kv_heads) dim], the fused projection -> q and k, which are columns of it, normalised and rotated."""
+
+    @staticmethod
+    def forward(ctx, x, heads, kv_heads, q_gain, k_gain, table, positions, eps):
+        rows, dim = x.shape[0], q_gain.numel()
+        q, k = x[:, :heads * dim].view(rows, heads, dim), x[:, heads * dim:(heads + kv_heads) * dim].view(rows, kv_heads, dim)
+        ctx.save_for_backward(x, q_gain, k_gain, table, positions)
+        ctx.how = heads, kv_heads, eps
+        return S.norm_rotate(q, k, q_gain, k_gain, table, positions, eps)
+
+    @staticmethod
+    def backward(ctx, dq_out, dk_out):
+        x, q_gain, k_gain, table, positions = ctx.saved_tensors
+        heads, kv_heads, eps = ctx.how
+        rows, dim = x.shape[0], q_gain.numel()
+        q, k = x[:, :heads * dim].view(rows, heads, dim), x[:, heads * dim:(heads + kv_heads) * dim].view(rows, kv_heads, dim)
+        dq, dk, dq_gain, dk_gain = S.norm_rotate_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, q_gain, k_gain, table, positions, eps)
+        dx = torch.zeros_like(x)
+        dx[:, :heads * dim], dx[:, heads * dim:(heads + kv_heads) * dim] = dq.view(rows, -1), dk.view(rows, -1)
+        return dx, None, None, dq_gain.to(q_gain.dtype), dk_gain.to(k_gain.dtype), None, None, None
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, bias, bias_map, causal, lengths):
+        how = dict(bias_map=bias_map, causal=causal, q_lengths=lengths, k_lengths=lengths)
+        out, lse = S.attention(q, k, v, bias, **how)
+        ctx.save_for_backward(q, k, v, out, lse, bias)
+        ctx.how = how
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, lse, bias = ctx.saved_tensors
+        return (*S.attention_backward(dout.contiguous(), q, k, v, out, lse, bias, **ctx.how), None, None, None)
+
+
+class _DropoutAdd(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, bias, residual, p, seed, step, site):
+        ctx.how, ctx.types = (p, seed, step, site), (x.dtype, bias.dtype)
+        return S.dropout_add(x, bias, residual, p, seed, step, site)
+
+    @staticmethod
+    def backward(ctx, dout):
+        dout = dout.contiguous()
+        dx, dbias = S.dropout_add_backward(dout, ctx.types[0], *ctx.how)
+        return dx, dbias.to(ctx.types[1]), dout, None, None, None, None
+
+
+class Cache:
+    """Keys and values of up to `most` tokens of each sequence, [batch, most, kv_heads, dim], and how many there are."""
+
+    def __init__(self, block, batch, most):
+        shape, w = (batch, most, block.kv_heads, block.dim), block.w_qkv
+        self.k, self.v = (torch.empty(shape, dtype=w.dtype, device=w.device) for _ in range(2))
+        self.lengths, self.held, self.most = torch.zeros(batch, dtype=torch.int32, device=w.device), 0, most
+
+
+class AttentionBlock(torch.nn.Module):
+    def __init__(self, d_model, heads, kv_heads=None, head_dim=64, buckets=32, reach=128, most_positions=4096, p=0.1, seed=0, site=0, eps=1e-6, dtype=torch.bfloat16, device="cuda:0"):
+        super().__init__()
+        self.heads, self.kv_heads, self.dim, self.p, self.seed, self.site, self.eps = heads, kv_heads or heads, head_dim, p, seed, site, eps
+        new = lambda t: torch.nn.Parameter(t.to(dtype).to(device))
+        g = torch.Generator().manual_seed(seed)
+        self.w_qkv = new(torch.randn((heads + 2 * self.kv_heads) * head_dim, d_model, generator=g) * d_model ** -0.5)
+        self.w_out = new(torch.randn(d_model, heads * head_dim, generator=g) * (heads * head_dim) ** -0.5)
+        self.b_out, self.q_gain, self.k_gain = new(torch.zeros(d_model)), new(torch.ones(head_dim)), new(torch.ones(head_dim))
+        self.bias = new(torch.zeros(buckets, heads))
+        self.register_buffer("bias_map", S.relative_buckets(buckets, reach, True, device))
+        self.register_buffer("table", S.rotation_table(most_positions, head_dim, device=device))
+
+    def forward(self, x, lengths=None, step=None):
+        """x [batch, tokens, d], lengths int32 [batch] or None; step: the training step that draws the dropout's mask, None: no dropout."""
+        b, t, d = x.shape
+        nq, nk = self.heads * self.dim, self.kv_heads * self.dim
+        qkv = torch.nn.functional.linear(x.reshape(b * t, d).to(self.w_qkv.dtype), self.w_qkv)
+        positions = torch.arange(t, dtype=torch.int32, device=x.device).repeat(b)
+        q, k = _NormRotate.apply(qkv, self.heads, self.kv_heads, self.q_gain, self.k_gain, self.table, positions, self.eps)
+        q, k, v = q.view(b, t, self.heads, self.dim), k.view(b, t, self.kv_heads, self.dim), qkv[:, nq + nk:].view(b, t, self.kv_heads, self.dim)
+        o = _Attention.apply(q, k, v, self.bias, self.bias_map, True, lengths)
+        y = torch.nn.functional.linear(o.reshape(b * t, nq), self.w_out)
+        return _DropoutAdd.apply(y, self.b_out, x.reshape(b * t, d), 0.0 if step is None else self.p, self.seed, step or 0, self.site).view(b, t, d)
+
+    @torch.no_grad()
+    def extend(self, x, cache):
+        """The next tokens x [batch, tokens, d] (one, or a prompt) of sequences whose earlier ones `cache` holds: their results, and the cache has them too."""
+        b, t, d = x.shape
+        if cache.lengths.numel() != b or cache.held + t > min(cache.most, self.table.shape[0]):
+            raise ValueError(f"{b} sequences of {cache.held} + {t} tokens: the cache is for {cache.lengths.numel()} of {cache.most}, the table of angles for {self.table.shape[0]} positions")
+        nq, nk = self.heads * self.dim, self.kv_heads * self.dim
+        flat = x.reshape(b * t, d)
+        qkv = torch.nn.functional.linear(flat.to(self.w_qkv.dtype), self.w_qkv)
+        positions = (cache.lengths[:, None] + torch.arange(t, dtype=torch.int32, device=x.device)).view(-1)
+        q, k = S.norm_rotate(qkv[:, :nq].view(b * t, self.heads, self.dim), qkv[:, nq:nq + nk].view(b * t, self.kv_heads, self.dim), self.q_gain, self.k_gain, self.table, positions, self.eps)
+        at = torch.arange(b, device=x.device).repeat_interleave(t), positions.long()
+        cache.k[at], cache.v[at] = k, qkv[:, nq + nk:].view(b * t, self.kv_heads, self.dim)
+        start, cache.lengths, cache.held = cache.lengths, cache.lengths + t, cache.held + t
+        o, _ = S.attention(q.view(b, t, self.heads, self.dim), cache.k, cache.v, self.bias, self.bias_map, causal=True, k_lengths=cache.lengths, q_start=start)
+        y = torch.nn.functional.linear(o.view(b * t, nq), self.w_out)
+        return S.dropout_add(y, self.b_out, flat, 0.0, self.seed, 0, self.site).view(b, t, d)
+
+
+def _recall(vocab, batch, tokens, g):
+    """A random sequence whose second half repeats its first: what follows a token is what followed it before."""
+    half = torch.randint(0, vocab, (batch, tokens // 2), generator=g)
+    return torch.cat([half, half], 1).cuda()
+
+
+def train(steps=300, batch=32, tokens=64, d_model=128, heads=4, kv_heads=2, vocab=32, dtype=torch.bfloat16, rate=3e-3, seed=1):
+    """Two blocks that learn to repeat a sequence; returns (embedding, blocks, losses): the mean loss of the second halves, step by step."""
+    g = torch.Generator().manual_seed(seed)
+    table = torch.nn.Parameter(torch.randn(vocab, d_model, generator=g).cuda())
+    head = torch.nn.Parameter((torch.randn(vocab, d_model, generator=g) * d_model ** -0.5).cuda())
+    blocks = [AttentionBlock(d_model, heads, kv_heads, head_dim=32, p=0.05, seed=seed, site=i, dtype=dtype) for i in range(2)]
+    opt = torch.optim.Adam([table, head] + [p for b in blocks for p in b.parameters()], lr=rate, eps=1e-6)
+    losses = []
+    for step in range(steps):
+        ids = _recall(vocab, batch, tokens, g)
+        x = table[ids]
+        for block in blocks:
+            x = block(x, step=step)
+        logits = torch.nn.functional.linear(x, head)[:, tokens // 2 - 1:-1]
+        loss = torch.nn.functional.cross_entropy(logits.reshape(-1, vocab), ids[:, tokens // 2:].reshape(-1))
+        opt.zero_grad(set_to_none=True)
+        loss.backward()
+        opt.step()
+        losses.append(loss.detach())
+    return (table.detach(), head.detach()), blocks, torch.stack(losses).cpu()
+
+
+@torch.no_grad()
+def answer(ends, blocks, prompt, tokens):
+    """`tokens` most likely tokens behind prompt [batch, n], one at a time over the blocks' caches."""
+    table, head = ends
+    caches = [Cache(block, prompt.shape[0], prompt.shape[1] + tokens) for block in blocks]
+    ids, said = prompt, []
+    for _ in range(tokens):
+        x = table[ids]
+        for block, cache in zip(blocks, caches):
+            x = block.extend(x, cache)
+        ids = torch.nn.functional.linear(x[:, -1:], head).argmax(-1)
+        said.append(ids)
+    return torch.cat(said, 1)
+
+
+def main(argv=None):
+    a = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    a.add_argument("--steps", type=int, default=300)
+    a.add_argument("--tokens", type=int, default=64)
+    a.add_argument("--f32", action="store_true")
+    o = a.parse_args(argv)
+    dtype = torch.float32 if o.f32 else torch.bfloat16
+    train(3, tokens=o.tokens, dtype=dtype)
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    ends, blocks, losses = train(o.steps, tokens=o.tokens, dtype=dtype)
+    t1 = time.perf_counter()
+    ids = _recall(ends[0].shape[0], 32, o.tokens, torch.Generator().manual_seed(7))
+    n = o.tokens // 2
+    said = answer(ends, blocks, ids[:, :n + 1], n - 1)
+    torch.cuda.synchronize()
+    t2 = time.perf_counter()
+    print(json.dumps({"steps": o.steps, "first_loss": float(losses[:10].mean()), "last_loss": float(losses[-10:].mean()), "ms_per_step": 1e3 * (t1 - t0) / o.steps,
+                      "repeated_right": float((said == ids[:, n + 1:]).float().mean()), "ms_per_token": 1e3 * (t2 - t1) / max(n - 1, 1)}))
+
+
+if __name__ == "__main__":
+    main()

@@ -454,3 +454,72 @@ def test_dropout_keeps_its_share_and_repeats_nothing(S):
     w = debug_philox(ctr, (1, 0))
     assert (w[0] != w[1]).all()
     assert [bool(v) for v in masks[0][0, :4]] == [int(v) >= 1 << 30 for v in w[0]]
+
+
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(9, 8193), (70, 8192), (3, 20011)])
+def test_dropout_of_long_rows(S, dtype, rows, cols):
+    """Rows in one block of the gradient's pass, and over several."""
+    g = _gen(cols)
+    x, bias, res, dout = _normal(g, rows, cols, dtype=dtype), _normal(g, cols, dtype=dtype), _normal(g, rows, cols), _normal(g, rows, cols)
+    key = (0.2, 11, 2, 1)
+    keep = R.keep_mask(rows, cols, *key)
+    R.check(S.dropout_add(x, bias, res, *key), res.cpu().double() + torch.where(keep, (x.cpu().double() + bias.cpu().double()) / 0.8, 0.0), "out")
+    dx, db = S.dropout_add_backward(dout, dtype, *key)
+    want = torch.where(keep, dout.cpu().double() / 0.8, 0.0)
+    R.check(dx, want, "dx")
+    R.check(db, want.sum(0), "dbias")
+
+
+# ------------------------------------------------------------------------------------------------ batches, slices, graphs
+@TYPES
+@pytest.mark.parametrize("batch", [70, 1030])
+def test_one_token_of_many_sequences(S, dtype, batch):
+    """More sequences than lanes, and more than the tiles are counted for; lengths from nothing to the whole cache."""
+    q, k, v, dout, how = _inputs(dtype, batch, 1, 2000, 8, 1, 8, 8, 30, True, seed=batch)
+    lengths = torch.randint(0, 2001, (batch,), generator=_gen(batch + 1), dtype=torch.int32)
+    lengths[:3] = torch.tensor([0, 2000, 1], dtype=torch.int32)
+    how.update(k_lengths=lengths.cuda(), q_start=lengths.cuda() - 1)
+    _compare(S, q, k, v, dout, how, grads=False)
+
+
+@TYPES
+@pytest.mark.parametrize("dim,n_k", [(64, 64), (128, 33), (32, 130)])
+def test_many_queries_over_few_keys(S, dtype, dim, n_k):
+    """dk and dv of few blocks, which are summed from slices of their queries."""
+    q, k, v, dout, how = _inputs(dtype, 1, 700, n_k, 4, 2, dim, 8, 20, False, seed=n_k)
+    _compare(S, q, k, v, dout, how)
+    how.update(causal=True, q_start=torch.tensor([-300], dtype=torch.int32, device="cuda"), q_lengths=torch.tensor([611], dtype=torch.int32, device="cuda"))
+    _compare(S, q, k, v, dout, how)
+
+
+def test_in_a_graph(S):
+    """Every operator captured once and replayed on new inputs, with the caller's own work between the replays."""
+    g = _gen(3)
+    new = lambda: (_normal(g, 300, 6 * 64, dtype=BF16), _normal(g, 300, 256, dtype=F32), _normal(g, 300, 4, 64, dtype=BF16))
+    x, res, dout = new()
+    gain, bias, drop = _normal(g, 64, dtype=BF16), _normal(g, 16, 4, dtype=BF16), _normal(g, 256, dtype=BF16)
+    table, at, m = S.rotation_table(512, 64), torch.arange(300, dtype=torch.int32, device="cuda"), S.relative_buckets(16, 50, True)
+
+    def work():
+        q, k, v = x[:, :256].view(300, 4, 64), x[:, 256:320].view(300, 1, 64), x[:, 320:].view(1, 300, 1, 64)
+        rq, rk = (t.view(1, 300, -1, 64) for t in S.norm_rotate(q, k, gain, gain, table, at))
+        out, lse = S.attention(rq, rk, v, bias, m, causal=True)
+        few, _ = S.attention(rq[:, -1:], rk, v, bias, m)
+        y = S.dropout_add(out.view(300, 256), drop, res, 0.1, 1, 2, 3)
+        dx, ddrop = S.dropout_add_backward(y, BF16, 0.1, 1, 2, 3)
+        grads = S.attention_backward(dout.view(1, 300, 4, 64), rq, rk, v, out, lse, bias, m, causal=True)
+        back = S.norm_rotate_backward(grads[0][0], grads[1][0], q, k, gain, gain, table, at)
+        return (rq, rk, out, lse, few, y, dx, ddrop, *grads, *back)
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = work()
+    for _ in range(4):
+        for t, n in zip((x, res, dout), new()):
+            t.copy_(n)
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(held, work())):
+            assert torch.equal(a, b), i
