@@ -125,6 +125,47 @@ template <typename T, int DH> __device__ __forceinline__ f32x16 rows_product(con
   return acc;
 }
 
+// The same with the lanes' own rows in LDS, a wave's fragments one behind the other: for kernels that lack the registers.
+template <typename T, int DH> __device__ __forceinline__ void put_own(unsigned char* own, const Own<T, DH>& o, int lane) {
+#pragma unroll
+  for (int s = 0; s < (int)(sizeof(o.f) / sizeof(o.f[0])); ++s) *reinterpret_cast<u32x4_t*>(own + s * 1024 + lane * 16) = __builtin_bit_cast(u32x4_t, o.f[s]);
+}
+template <int DH, typename O> __device__ __forceinline__ f32x16 rows_product_chunks(const unsigned char* lds, int row0, const O& own, int lane) {
+  const int l32 = lane & 31, half = lane >> 5;
+  f32x16 acc = zeros16();
+  const unsigned char* row = lds + (row0 + l32) * (DH * 2);
+  const int t = turn_of<bf16_bits, DH>(l32);
+#pragma unroll
+  for (int c = 0; c < DH / 16; c += 4) {
+    bf16x8 a[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) a[s] = *reinterpret_cast<const bf16x8*>(row + (((2 * (c + s) + half) ^ t) << 4));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s], own.f[c + s], acc, 0, 0, 0);
+  }
+  return acc;
+}
+template <int DH> __device__ __forceinline__ f32x16 rows_product_lds(const unsigned char* lds, int row0, const unsigned char* own, int lane) {
+  const int l32 = lane & 31, half = lane >> 5;
+  f32x16 acc = zeros16();
+  const unsigned char* row = lds + (row0 + l32) * (DH * 2);
+  const int t = turn_of<bf16_bits, DH>(l32);
+#pragma unroll
+  for (int c = 0; c < DH / 16; c += 4) {
+    bf16x8 a[4], b[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      a[s] = *reinterpret_cast<const bf16x8*>(row + (((2 * (c + s) + half) ^ t) << 4));
+      b[s] = *reinterpret_cast<const bf16x8*>(own + (c + s) * 1024 + lane * 16);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s], b[s], acc, 0, 0, 0);
+  }
+  return acc;
+}
+
 // A tile as the second kind of product takes it.
 template <typename T> struct Tile;
 template <> struct Tile<bf16_bits> { uint32_t w[8]; };
@@ -199,9 +240,37 @@ template <typename T, int DH> __device__ __forceinline__ void columns_product(f3
   }
 }
 
+// The same for heads of 128 in bf16, 16 rows at a time, for kernels that lack the registers.
+__device__ __forceinline__ void columns_product_late(f32x16 (&acc)[4], const unsigned char* lds, int row0, const Tile<bf16_bits>& tile, int lane) {
+  const int i16 = lane & 15, piece = ((lane & 16) >> 3) + ((i16 & 3) >> 1), down = (i16 >> 2) + 4 * (lane >> 5);
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds + (uint32_t)((row0 + down) * 256 + (i16 & 1) * 8);
+  const int t0 = turn_of<bf16_bits, 128>(down), t1 = turn_of<bf16_bits, 128>(down + 8);
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    u32x2_t lo[4], hi[4];
+    uint32_t a[4], b[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      a[f] = at + (uint32_t)(((4 * f + piece) ^ t0) << 4);
+      b[f] = at + (uint32_t)(((4 * f + piece) ^ t1) << 4);
+    }
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%17\n\tds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %3, %11 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%17\n\tds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3])
+                 : "v"(a[0]), "v"(b[0]), "v"(a[1]), "v"(b[1]), "v"(a[2]), "v"(b[2]), "v"(a[3]), "v"(b[3]), "n"(ks * 4096), "n"(ks * 4096 + 2048) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+    const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4_t{tile.w[4 * ks], tile.w[4 * ks + 1], tile.w[4 * ks + 2], tile.w[4 * ks + 3]});
+#pragma unroll
+    for (int f = 0; f < 4; ++f) acc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4_t{lo[f][0], lo[f][1], hi[f][0], hi[f][1]}), w, acc[f], 0, 0, 0);
+  }
+}
+
 // The same sum without the matrix instructions, of the pairs that are seen alone: 0 x infinity and 0 x NaN of hidden pairs stay out of it.  Only taken where a result
 // was not finite: then by tiles with hidden pairs.
-template <typename T, int DH> __device__ __forceinline__ void columns_exactly(f32x16 (&acc)[DH / 32], const unsigned char* lds, int row0, const float (&coef)[16], uint32_t seen, int lane) {
+template <typename T, int DH, int N> __device__ __forceinline__ void columns_exactly(f32x16 (&acc)[N], const unsigned char* lds, int row0, const float (&coef)[16], uint32_t seen, int lane, int f0 = 0) {
   constexpr int bytes = DH * (int)sizeof(T);
   const int half = lane >> 5, l32 = lane & 31;
 #pragma unroll 1
@@ -214,10 +283,10 @@ template <typename T, int DH> __device__ __forceinline__ void columns_exactly(f3
     const bool on = (__shfl((int)seen, from, 64) >> reg) & 1;
     const unsigned char* at = lds + (row0 + r) * bytes;
 #pragma unroll
-    for (int f = 0; f < DH / 32; ++f)
+    for (int f = 0; f < N; ++f)
 #pragma unroll
       for (int v = 0; v < 16; v += 4) {
-        const int byte = (32 * f + 2 * v + 4 * half) * (int)sizeof(T);
+        const int byte = (32 * (f0 + f) + 2 * v + 4 * half) * (int)sizeof(T);
         const T* y = reinterpret_cast<const T*>(at + ((((byte >> 4) ^ t) << 4) | (byte & 15)));
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[f][v + i] = on ? __builtin_fmaf(x, as_float(y[i]), acc[f][v + i]) : acc[f][v + i];
@@ -274,10 +343,19 @@ __device__ __forceinline__ Sequence sequence_of(const zgr_attention& h, int b) {
   return q;
 }
 
+// The lane's number, taken anew wherever it is asked for: it holds no register in between.
+__device__ __forceinline__ int lane_now() {
+  int all = -1;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+s"(all));
+#endif
+  return __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
+}
+
 // The bias of one head by relative position, in units of log2, kBiasPad places beyond reach on either side; a bucket that the table doesn't have gives NaN.
-template <typename T> __device__ __forceinline__ void stage_bias(float* lds, const zgr_attention& h, int head) {
+template <typename T, int NW> __device__ __forceinline__ void stage_bias(float* lds, const zgr_attention& h, int head, int wave) {
   const int n = 2 * h.bias_reach + 1 + 2 * kBiasPad;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+  for (int i = wave * 64 + lane_now(); i < n; i += 64 * NW) {
     const int bucket = h.bias_map[min(max(i - kBiasPad, 0), 2 * h.bias_reach)];
     lds[i] = bucket >= 0 && bucket < h.bias_buckets ? as_float(((const T*)h.bias)[(int64_t)bucket * h.n_head + head]) * kLog2e : __uint_as_float(0x7FC00000u);
   }
@@ -312,7 +390,7 @@ template <typename T> __device__ __forceinline__ const T* row_at(const zgr_heads
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
-// Result [entries x lanes] to the lanes' rows.
+// Result [entries x lanes] to the lanes' rows; by = 0: zeros, whatever the sums hold.
 template <typename T, int DH> __device__ __forceinline__ void store_columns(T* row, const f32x16 (&acc)[DH / 32], float by, int half, int dim) {
 #pragma unroll
   for (int f = 0; f < DH / 32; ++f)
@@ -320,7 +398,9 @@ template <typename T, int DH> __device__ __forceinline__ void store_columns(T* r
     for (int v = 0; v < 16; v += 4) {
       const int c = 32 * f + 2 * v + 4 * half;
       if (c >= dim) continue;
-      const float x[4] = {acc[f][v] * by, acc[f][v + 1] * by, acc[f][v + 2] * by, acc[f][v + 3] * by};
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = by == 0.f ? 0.f : acc[f][v + i] * by;
       if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(row + c) = f32x4_t{x[0], x[1], x[2], x[3]};
       else *reinterpret_cast<u32x2_t*>(row + c) = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
     }
@@ -346,6 +426,21 @@ __device__ __forceinline__ void block_barrier() {      // without __syncthreads'
 __device__ __forceinline__ int uniform_of(int v) { return __builtin_amdgcn_readfirstlane(v); }
 constexpr int kStatRows = 256;                              // rows of the backward pass's statistics are padded to whole blocks
 __host__ __device__ inline int64_t stat_rows(int n_q) { return ((int64_t)n_q + kStatRows - 1) / kStatRows * kStatRows; }
+
+// Whether `mine` holds in any lane of the block.  lds: whose transfers and reads are done in every wave that has come here (its first words are written).
+template <int NW> __device__ __forceinline__ bool any_of_block(bool mine, unsigned char* lds, int wave) {
+  int* flags = reinterpret_cast<int*>(lds);
+  const bool any = __builtin_amdgcn_ballot_w64(mine) != 0;
+  __syncthreads();
+  if (lane_now() == 0) flags[wave] = any;
+  __syncthreads();
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) all |= flags[w];
+  const bool yes = uniform_of(all) != 0;
+  if (yes) __syncthreads();                                 // the next pass fills the same place
+  return yes;
+}
 
 // Which queries a block works on.  Under the causal mask a block's work grows with its position and a wave's with its queries': blocks go longest first, and with eight waves, of
 // which w and w + 4 share a SIMD, the upper four take their queries in reverse order.
@@ -403,7 +498,7 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
       for (int st = 0; st < Sh::ring - 1; ++st) stage(st);
     if (!careful) {
       load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, qi < sq.n_q);
-      if (biased) stage_bias<T>(by_delta, how, h);
+      if (biased) stage_bias<T, NW>(by_delta, how, h, wave);
     }
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
@@ -474,7 +569,7 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
       for (int v = 0; v < 16; ++v) bad |= !finite(o[f][v]);
-    return __syncthreads_or(bad && qi < sq.n_q);
+    return any_of_block<NW>(bad && qi < sq.n_q, lds, wave);
   };
   if (pass(std::false_type())) pass(std::true_type());
   if (qi >= how.n_q) return;
@@ -831,7 +926,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
       Own<T, DH> o;
       load_own<T, DH>(o, row_at<T>(a.out, b, qi, h), half, how.head_dim, valid);
       dot = both_halves(dot_own<T, DH>(o, d));
-      if (biased) stage_bias<T>(by_delta, how, h);
+      if (biased) stage_bias<T, NW>(by_delta, how, h, wave);
     }
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) dq[f] = zeros16();
@@ -917,7 +1012,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
       for (int v = 0; v < 16; ++v) bad |= !finite(dq[f][v]);
-    return __syncthreads_or(bad && valid);
+    return any_of_block<NW>(bad && valid, lds, wave);
   };
   if (pass(std::false_type())) pass(std::true_type());
   if (half == 0) {
@@ -962,8 +1057,11 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
 }
 
 // ------------------------------------------------------------------------------------------------ backward: dk, dv
+// Two waves on a SIMD are worth more here than anything that the registers could hold: heads of 128 in bf16, whose dk and dv alone take 128 registers, keep their rows of v in LDS, read their
+// operands in parts and redo what is not finite 32 entries at a time (with everything in registers and one wave: backward of 2 x 2047 tokens, 32 heads of 128 on 8, 445 us, so 372).
+template <typename T, int DH> constexpr bool kOwnInLds = sizeof(T) == 2 && DH == 128;
 template <typename T, int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ stats, Grid grid, float* __restrict__ part) {
+__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<T, DH>) ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ stats, Grid grid, float* __restrict__ part) {
   using Sh = Shape<T, DH>;
   constexpr int KB = 32 * NW, QB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -975,7 +1073,9 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
   float* rows_stats = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);      // [ring][2][64]
-  float* by_delta = rows_stats + Sh::ring * 128;
+  constexpr bool own_in_lds = kOwnInLds<T, DH>;
+  unsigned char* own_v = lds + Sh::ring * (2 * Sh::bytes + 512) + wave * (32 * DH * (int)sizeof(T));
+  float* by_delta = rows_stats + Sh::ring * 128 + (own_in_lds ? NW * 32 * DH * (int)sizeof(T) / 4 : 0);
   const bool biased = how.bias != nullptr;
   const int reach = how.bias_reach, causal = how.causal;
   const int block_k0 = kb * KB, k0 = block_k0 + group_of<NW>(wave, causal) * 32, kj = k0 + l32;
@@ -993,6 +1093,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
   struct At { int st, h, first; };                          // a stage's number, head and first query
   auto stage = [&](const At& at) {
     unsigned char* to = lds + at.st % Sh::ring * (2 * Sh::bytes);
+    const int lane = own_in_lds ? lane_now() : tid & 63;
     stage_rows<T, DH, QB, NW>(to, row_at<T>(a.q, b, 0, at.h), a.q.token, row_at<T>(a.dout, b, 0, at.h), a.dout.token, at.first, sq.n_q - 1, how.head_dim, wave, lane);
     if (wave < 2) {                                         // the rows' statistics (64 of them, of which a stage of 32 rows uses half)
       const float* src = stats + ((int64_t)b * how.n_head + at.h) * 2 * n_stats + wave * n_stats + min((int64_t)at.first + lane, n_stats - 1);
@@ -1009,8 +1110,26 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
   const float scale = how.scale * kLog2e;
   Own<T, DH> k, vv;
   f32x16 dk[DH / 32], dv[DH / 32];
-  auto pass = [&](auto again) -> bool {                     // whether a row's result is not finite; again: then once more, with hidden pairs left out of the products (columns_exactly)
+  auto store = [&](const auto& ck, const auto& cv, int c0) { // entries from c0 on
+    constexpr int N = sizeof(ck) / sizeof(ck[0]) * 32;
+    const int lane = lane_now(), half = lane >> 5, kj = k0 + (lane & 31);
+    const bool valid = kj < sq.n_k;
+    if (kj >= how.n_k) return;
+    if (grid.parts > 1) {                                   // [2][slices][units][n_k][head_dim], for heads_slices_kernel
+      const int64_t rows = (int64_t)grid.units * how.n_k, row = (int64_t)place.unit * how.n_k + kj;
+      store_columns<float, N>(part + (place.part * rows + row) * how.head_dim + c0, ck, valid ? how.scale : 0.f, half, how.head_dim - c0);
+      store_columns<float, N>(part + ((grid.parts + place.part) * rows + row) * how.head_dim + c0, cv, valid ? 1.0f : 0.f, half, how.head_dim - c0);
+    } else {
+      store_columns<T, N>(const_cast<T*>(row_at<T>(a.dk, b, kj, hk)) + c0, ck, valid ? how.scale : 0.f, half, how.head_dim - c0);
+      store_columns<T, N>(const_cast<T*>(row_at<T>(a.dv, b, kj, hk)) + c0, cv, valid ? 1.0f : 0.f, half, how.head_dim - c0);
+    }
+  };
+  // whether a row's result is not finite; again: then once more, 32 entries from 32 f on at a time, with hidden pairs left out of the products (columns_exactly)
+  auto pass = [&](auto again, int f0) -> bool {
     constexpr bool careful = decltype(again)::value;
+    const int lane = lane_now(), l32 = lane & 31, half = lane >> 5, kj = k0 + l32;      // anew: addresses of the second pass aren't kept in registers through the first
+    const bool valid = kj < sq.n_k;
+    f32x16 ck[1] = {zeros16()}, cv[1] = {zeros16()};
     At ahead{0, hk * group + first_head, first_query};
     if (stages)
 #pragma unroll
@@ -1018,14 +1137,16 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
     if (!careful) {
       load_own<T, DH>(k, row_at<T>(a.k, b, kj, hk), half, how.head_dim, valid);
       load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
+      if constexpr (own_in_lds) put_own<T, DH>(own_v, vv, lane);
     }
+    if (!careful)
 #pragma unroll
-    for (int f = 0; f < DH / 32; ++f) dk[f] = dv[f] = zeros16();
+      for (int f = 0; f < DH / 32; ++f) dk[f] = dv[f] = zeros16();
     At here{0, hk * group + first_head, first_query};
     for (int st = 0; st < stages; ++st, next(here)) {
       if ((st == 0 || here.first == qbegin) && biased) {    // another head
         if (st) block_barrier();
-        stage_bias<T>(by_delta, how, here.h);
+        stage_bias<T, NW>(by_delta, how, here.h, wave);
       }
       if (wave < 2) transfers_upto<(PER + 1) * (Sh::ring - 2)>();
       else transfers_upto<PER * (Sh::ring - 2)>();
@@ -1039,12 +1160,19 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
         const int q0 = here.first + ql, pos0 = sq.start + q0;
         if (q0 >= sq.n_q) break;
         if (q0 + 31 < wave_qbegin) continue;
-        if (careful) load_own<T, DH>(k, row_at<T>(a.k, b, kj, hk), half, how.head_dim, valid);
-        const f32x16 s = rows_product<T, DH>(Q, ql, k, l32, half);
-        if (careful) load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
-        const f32x16 dp = rows_product<T, DH>(D, ql, vv, l32, half);
+        f32x16 s, dp;
+        if constexpr (own_in_lds && !careful) s = rows_product_chunks<DH>(Q, ql, k, lane);
+        else {
+          if (careful) load_own<T, DH>(k, row_at<T>(a.k, b, kj, hk), half, how.head_dim, valid);
+          s = rows_product<T, DH>(Q, ql, k, l32, half);
+        }
+        if constexpr (own_in_lds) dp = rows_product_lds<DH>(D, ql, own_v, lane);
+        else {
+          if (careful) load_own<T, DH>(vv, row_at<T>(a.v, b, kj, hk), half, how.head_dim, valid);
+          dp = rows_product<T, DH>(D, ql, vv, l32, half);
+        }
         Columns<T, DH> cols;
-        if (!careful) load_columns<T, DH>(cols, D, ql, lane);
+        if (!careful && !own_in_lds) load_columns<T, DH>(cols, D, ql, lane);
         const bool whole = k0 + 31 < sq.n_k && q0 + 31 < sq.n_q && (!causal || k0 + 31 <= pos0);
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;
         float p[16], ds[16];
@@ -1060,6 +1188,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
 #pragma unroll
           for (int v = 0; v < 16; ++v) p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, flat - lses[ql + 8 * (v >> 2) + (v & 3)]));
         }
+        if (own_in_lds) __builtin_amdgcn_sched_barrier(0);     // the statistics' reads not all at once
 #pragma unroll
         for (int v = 0; v < 16; ++v) ds[v] = p[v] * (dp[v] - lses[64 + ql + 8 * (v >> 2) + (v & 3)]);
         uint32_t seen = 0xFFFF;
@@ -1074,45 +1203,48 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 ? 1 : 2) heads_
             ds[v] = on ? ds[v] : 0.f;
           }
         }
-        Tile<T> tp, td;
-#pragma unroll
-        for (int v = 0; v < 16; v += 2) {
-          put_pair(tp, v, p[v], p[v + 1]);
-          put_pair(td, v, ds[v], ds[v + 1]);
-        }
-        if (careful && !whole) {
-          columns_exactly<T, DH>(dv, D, ql, p, seen, lane);
-          columns_exactly<T, DH>(dk, Q, ql, ds, seen, lane);
+        if constexpr (careful) {
+          columns_exactly<T, DH>(cv, D, ql, p, seen, lane, f0);
+          columns_exactly<T, DH>(ck, Q, ql, ds, seen, lane, f0);
         } else {
-          if (careful) load_columns<T, DH>(cols, D, ql, lane);
-          columns_product<T, DH>(dv, cols, tp);
-          load_columns<T, DH>(cols, Q, ql, lane);
-          columns_product<T, DH>(dk, cols, td);
+          Tile<T> tp, td;
+#pragma unroll
+          for (int v = 0; v < 16; v += 2) {
+            put_pair(tp, v, p[v], p[v + 1]);
+            put_pair(td, v, ds[v], ds[v + 1]);
+          }
+          if constexpr (own_in_lds) {
+            columns_product_late(dv, D, ql, tp, lane);
+            columns_product_late(dk, Q, ql, td, lane);
+          } else {
+            columns_product<T, DH>(dv, cols, tp);
+            load_columns<T, DH>(cols, Q, ql, lane);
+            columns_product<T, DH>(dk, cols, td);
+          }
         }
       }
     }
     transfers_upto<0>();
-    if (careful) return false;
+    if constexpr (careful) {
+      store(ck, cv, 32 * f0);
+      __syncthreads();                                      // LDS is the next pass's
+      return false;
+    }
     bool bad = false;
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f)
 #pragma unroll
       for (int v = 0; v < 16; ++v) bad |= !finite(dk[f][v]) || !finite(dv[f][v]);
-    return __syncthreads_or(bad && valid);
+    return any_of_block<NW>(bad && valid, lds, wave);
   };
-  if (pass(std::false_type())) pass(std::true_type());
-  if (kj >= how.n_k) return;
-  if (!valid)
-#pragma unroll
-    for (int f = 0; f < DH / 32; ++f) dk[f] = dv[f] = zeros16();
-  if (grid.parts > 1) {                                     // [2][slices][units][n_k][head_dim], for heads_slices_kernel
-    const int64_t rows = (int64_t)grid.units * how.n_k, row = (int64_t)place.unit * how.n_k + kj;
-    store_columns<float, DH>(part + (place.part * rows + row) * how.head_dim, dk, how.scale, half, how.head_dim);
-    store_columns<float, DH>(part + ((grid.parts + place.part) * rows + row) * how.head_dim, dv, 1.0f, half, how.head_dim);
-    return;
-  }
-  store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dk, b, kj, hk)), dk, how.scale, half, how.head_dim);
-  store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dv, b, kj, hk)), dv, 1.0f, half, how.head_dim);
+  int again = pass(std::false_type(), 0);
+  if (!again) store(dk, dv, 0);
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(again));                           // one after the other, not an if and its else, for which the compiler keeps dk and dv through the second pass
+#endif
+  if (uniform_of(again))
+#pragma unroll 1
+    for (int f0 = 0; 32 * f0 < how.head_dim; ++f0) pass(std::true_type(), f0);
 }
 
 // dk and dv from their slices' sums, in the slices' order: four entries a thread.
@@ -1153,10 +1285,11 @@ __global__ void __launch_bounds__(1024) heads_dbias_kernel(zgr_attention how, co
   }
 }
 
+constexpr int kForwardWaves = 4, kQueryWaves = 4, kKeyWaves = 4;
 template <typename T, int DH> int ring_bytes() { return Shape<T, DH>::ring * 2 * Shape<T, DH>::bytes; }
 template <typename T, int DH> int forward_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + bias_bytes(how); }
 template <typename T, int DH, int NW> int dq_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + bias_bytes(how) + bias_places(how) * 4 * NW; }
-template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + Shape<T, DH>::ring * 128 * 4 + bias_bytes(how); }
+template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + Shape<T, DH>::ring * 128 * 4 + (kOwnInLds<T, DH> ? kKeyWaves * 32 * DH * (int)sizeof(T) : 0) + bias_bytes(how); }
 
 template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), int64_t blocks, int threads, int lds, hipStream_t s, A... args) {
   if (!blocks) return hipSuccess;                           // nothing of its kind
@@ -1166,7 +1299,6 @@ template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), i
   return hipGetLastError();
 }
 
-constexpr int kForwardWaves = 4, kQueryWaves = 4, kKeyWaves = 4;
 // Blocks of n rows, `parts` for each unit (a K/V head of a sequence).
 Grid grid_of(const zgr_attention& how, int n, int block, int parts) {
   Grid g;
@@ -1175,19 +1307,20 @@ Grid grid_of(const zgr_attention& how, int n, int block, int parts) {
   return g;
 }
 Grid query_grid(const zgr_attention& how, int waves) { return grid_of(how, how.n_q, 32 * waves, how.n_head / how.n_kv_head); }
-// Keys: a block walks the queries of every head of its unit.  Where that makes few blocks, whose longest would be waited for, they are cut into slices of equal length, up to some 512 blocks
-// in all: slices cost a write and a read of dk and dv in fp32 each.  2 x 2047 tokens, 32 heads of 128 on 8, backward: 626 us without, 447 cut in two, 477 in three; 4096 tokens, 16 heads of 64 on
-// 4: 682, 287 (four slices), 286 (eight); where 512 blocks are there already, a second slice took 144 us to 198.
+int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
+// Keys: a block walks the queries of every head of its unit.  Where that makes few blocks, whose longest would be waited for, they are cut into slices of equal length, up to as
+// many as the chip holds at once, or twice that under the causal mask, where their lengths differ: slices cost a write and a read of dk and dv in fp32 each.
+// Backward: 2 x 2047 tokens, 32 heads of 128 on 8 (256 blocks), 633 us without, 426 in two, 372 in four; 4096 tokens, 16 heads of 64 on 4 (128 blocks), 667, 278 (four) and 277 (eight); both
+// ways 1500 tokens, 8 heads of 64 (96 blocks), 139 and 104 (five); 8 x 512 tokens, 16 heads of 128 (512 blocks), 114, and in two 156.
 Grid key_grid(const zgr_attention& how) {
   Grid g = grid_of(how, how.n_k, 32 * kKeyWaves, 1);
   const int64_t blocks = (int64_t)g.units * g.ranks, walk = (int64_t)((how.n_q + 63) / 64) * (how.n_head / how.n_kv_head);
-  int slices = blocks ? (int)((512 + blocks - 1) / blocks) : 1;
-  if (slices > walk / 4) slices = (int)(walk / 4);
-  g.parts = slices < 1 ? 1 : slices;
+  const int64_t held = how.dtype == ZGR_F32 && how.head_dim > 32 ? 256 : 512, wanted = how.causal ? 2 * held : held;
+  int64_t slices = blocks ? (wanted + blocks / 2) / blocks : 1;
+  if (slices > walk / 4) slices = walk / 4;
+  g.parts = slices < 1 ? 1 : (int)slices;
   return g;
 }
-
-int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
 
 // Which of the two forward kernels: the sooner done by an estimate.  Blocks of queries walk all keys, 0.57 us (bf16, heads up to 64), 1.0 (128), 2.4 and 4.5 (fp32) a tile of 32, some
 // 768 blocks at a time.  Runs of tiles take 4 us for each 8 KiB tile of a worker's run, of which there are 2048 (1024), and 8 us more to begin with (the count, and the launch that joins
