@@ -365,24 +365,25 @@ __host__ __device__ inline int bias_bytes(const zgr_attention& h) { return (bias
 
 // What a block works on: `rank` counts the blocks of a head from the one with the most work (under the causal mask) to the one with the least, `part` the heads that share a unit's K and
 // V (or the slices of its work).  Consecutive block ids go round-robin to the 8 XCDs, each with an L2 of its own.  by_unit: each unit belongs to an XCD, and the blocks with the most work of
-// all its units go first, so that the short ones fill the gaps at the end; where that would leave XCDs with more units than others, every XCD gets an equal run of blocks, unit by unit.
-struct Grid { int units, parts, ranks, by_unit; };
+// all its units go first, so that the short ones fill the gaps at the end (paired: the first half, and the second half from its least on); where that would leave XCDs with more units than others, every XCD gets an equal run of blocks, unit by unit.
+struct Grid { int units, parts, ranks, by_unit, paired; };
 __host__ __device__ inline int64_t blocks_of(const Grid& g) {
   return g.by_unit ? (int64_t)8 * ((g.units + 7) / 8) * g.parts * g.ranks : ((int64_t)g.units * g.parts * g.ranks + 7) / 8 * 8;
 }
 struct Place { int unit, part, rank; };
+__device__ __forceinline__ int turned_rank(const Grid& g, int rank) { return g.paired && rank >= (g.ranks + 1) / 2 ? g.ranks - 1 - (rank - (g.ranks + 1) / 2) : rank; }
 __device__ __forceinline__ bool place_of_block(const Grid& g, Place& p) {
   const int xcd = blockIdx.x & 7;
   const uint32_t local = blockIdx.x >> 3;
   if (g.by_unit) {
     const uint32_t most = (uint32_t)(g.units + 7) / 8, j = local % most, rest = local / most;
-    p.unit = xcd + 8 * (int)j, p.part = (int)(rest % (uint32_t)g.parts), p.rank = (int)(rest / (uint32_t)g.parts);
+    p.unit = xcd + 8 * (int)j, p.part = (int)(rest % (uint32_t)g.parts), p.rank = turned_rank(g, (int)(rest / (uint32_t)g.parts));
     return p.unit < g.units;
   }
   const uint32_t each = (uint32_t)g.parts * (uint32_t)g.ranks, total = (uint32_t)g.units * each, q = total >> 3, rem = total & 7;
   if (local >= q + ((uint32_t)xcd < rem ? 1 : 0)) return false;
   const uint32_t at = (uint32_t)xcd * q + ((uint32_t)xcd < rem ? (uint32_t)xcd : rem) + local, rest = at % each;
-  p.unit = (int)(at / each), p.rank = (int)(rest / (uint32_t)g.parts), p.part = (int)(rest % (uint32_t)g.parts);
+  p.unit = (int)(at / each), p.rank = turned_rank(g, (int)(rest / (uint32_t)g.parts)), p.part = (int)(rest % (uint32_t)g.parts);
   return true;
 }
 
@@ -1070,7 +1071,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<
   Place place;
   if (!place_of_block(grid, place)) return;
   const int kb = place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const int wave = uniform_of(threadIdx.x >> 6);
   const Sequence sq = sequence_of(how, b);
   float* rows_stats = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);      // [ring][2][64]
   constexpr bool own_in_lds = kOwnInLds<T, DH>;
@@ -1078,8 +1079,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<
   float* by_delta = rows_stats + Sh::ring * 128 + (own_in_lds ? NW * 32 * DH * (int)sizeof(T) / 4 : 0);
   const bool biased = how.bias != nullptr;
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_k0 = kb * KB, k0 = block_k0 + group_of<NW>(wave, causal) * 32, kj = k0 + l32;
-  const bool valid = kj < sq.n_k;
+  const int block_k0 = kb * KB, k0 = block_k0 + group_of<NW>(wave, causal) * 32;
   // the first query that sees a key of the block, and of the wave
   int qbegin = causal ? max(0, block_k0 - sq.start) : 0, wave_qbegin = causal ? max(0, k0 - sq.start) : 0;
   if (block_k0 >= sq.n_k) qbegin = sq.n_q;
@@ -1093,7 +1093,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<
   struct At { int st, h, first; };                          // a stage's number, head and first query
   auto stage = [&](const At& at) {
     unsigned char* to = lds + at.st % Sh::ring * (2 * Sh::bytes);
-    const int lane = own_in_lds ? lane_now() : tid & 63;
+    const int lane = own_in_lds ? lane_now() : (int)threadIdx.x & 63;
     stage_rows<T, DH, QB, NW>(to, row_at<T>(a.q, b, 0, at.h), a.q.token, row_at<T>(a.dout, b, 0, at.h), a.dout.token, at.first, sq.n_q - 1, how.head_dim, wave, lane);
     if (wave < 2) {                                         // the rows' statistics (64 of them, of which a stage of 32 rows uses half)
       const float* src = stats + ((int64_t)b * how.n_head + at.h) * 2 * n_stats + wave * n_stats + min((int64_t)at.first + lane, n_stats - 1);
@@ -1304,9 +1304,17 @@ Grid grid_of(const zgr_attention& how, int n, int block, int parts) {
   Grid g;
   g.units = how.batch * how.n_kv_head, g.parts = parts, g.ranks = (n + block - 1) / block;
   g.by_unit = (g.units + 7) / 8 * 8 <= g.units + g.units / 8;
+  g.paired = 0;
   return g;
 }
-Grid query_grid(const zgr_attention& how, int waves) { return grid_of(how, how.n_q, 32 * waves, how.n_head / how.n_kv_head); }
+// Queries: where all blocks are on the chip at once, two to a compute unit, the shortest stand beside the longest (fp32, 2 x 2048 causal tokens, 16 heads of 64: 217 us forward, so 174; bf16 the same
+// either way, as a block's own tiles in turn are what is waited for).
+Grid query_grid(const zgr_attention& how, int waves) {
+  Grid g = grid_of(how, how.n_q, 32 * waves, how.n_head / how.n_kv_head);
+  const int64_t blocks = (int64_t)g.units * g.ranks * g.parts;
+  g.paired = how.causal && g.by_unit && blocks > 256 && blocks <= 512;
+  return g;
+}
 int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
 // Keys: a block walks the queries of every head of its unit.  Where that makes few blocks, whose longest would be waited for, they are cut into slices of equal length, up to as
 // many as the chip holds at once, or twice that under the causal mask, where their lengths differ: slices cost a write and a read of dk and dv in fp32 each.
