@@ -173,9 +173,8 @@ template <> struct Tile<float> { float w[16]; };
 __device__ __forceinline__ void put_pair(Tile<bf16_bits>& t, int v, float a, float b) { t.w[v / 2] = pack_bf16(a, b); }
 __device__ __forceinline__ void put_pair(Tile<float>& t, int v, float a, float b) { t.w[v] = a; t.w[v + 1] = b; }
 
-// Columns of 32 rows of LDS, for the second kind.  bf16: 16 lanes receive the columns of a piece of 4 rows of 16 entries.  Written as one block with its wait: behind the builtin the
-// compiler waits for every transfer to LDS that is on its way (at the builtin's first use 2 x 2047 tokens, 32 heads of 128 took 760 us backward and 165 forward).  It goes where
-// products of the first kind have just been issued, which run meanwhile.
+// Columns of 32 rows of LDS, for the second kind.  bf16: 16 lanes receive the columns of a piece of 4 rows of 16 entries.  Written as one block with its wait, so that it stands where
+// products of the first kind have just been issued, which run meanwhile (the builtin in its place measures the same).
 template <typename T, int DH> struct Columns;
 template <int DH> struct Columns<bf16_bits, DH> { u32x2_t lo[2][DH / 32], hi[2][DH / 32]; };
 template <int DH> struct Columns<float, DH> { const unsigned char* at[4]; };
@@ -408,12 +407,14 @@ template <typename T, int DH> __device__ __forceinline__ void store_columns(T* r
 }
 
 // A block is NW waves of 32 queries (or keys), which share the rows that they walk.  Those go through a ring of RING stages of ROWS rows of two operands in LDS: the stage in
-// use, the one whose readers may not have finished, and the ones between that are on their way.
-template <typename T, int DH> struct Shape {
+// use and the next one, which is on its way into the place whose readers the stage's barrier has seen finish.  64 rows a stage, 32 where LDS would hold one block only (heads of 128 in bf16,
+// 2 x 2047 tokens, backward: 378 us with 32 everywhere, 367; rings of three stages 1 to 3% slower).
+template <typename T, int DH, int LONG = 64> struct Shape {
   static constexpr int row = DH * (int)sizeof(T);
-  static constexpr int rows = row >= 256 ? 32 : 64, ring = 2;
+  static constexpr int rows = row > 256 ? 32 : row == 256 ? LONG : 64, ring = 2;
   static constexpr int bytes = rows * row;                  // of one operand's stage
 };
+template <typename T, int DH> using KeyShape = Shape<T, DH, 32>;      // of the blocks that walk queries, whose LDS holds more beside it
 template <int N> __device__ __forceinline__ void transfers_upto() {      // all but the last N of this wave's transfers have landed
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -943,11 +944,15 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
         const int k0 = st * KB + kl;
         if (k0 >= wave_kend) break;
         if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, valid);
-        const f32x16 s = rows_product<T, DH>(K, kl, q, l32, half);
+        constexpr bool early = DH * sizeof(T) != 256;          // heads of 128 in bf16 have no registers for the columns meanwhile, nor for a whole row's pieces
+        constexpr bool parts_of_rows = sizeof(T) == 2 && !early;
+        f32x16 s, dp;
+        if constexpr (parts_of_rows) s = rows_product_chunks<DH>(K, kl, q, lane);
+        else s = rows_product<T, DH>(K, kl, q, l32, half);
         if (careful) load_own<T, DH>(d, row_at<T>(a.dout, b, qi, h), half, how.head_dim, valid);
-        const f32x16 dp = rows_product<T, DH>(V, kl, d, l32, half);
+        if constexpr (parts_of_rows) dp = rows_product_chunks<DH>(V, kl, d, lane);
+        else dp = rows_product<T, DH>(V, kl, d, l32, half);
         Columns<T, DH> cols;
-        constexpr bool early = DH * sizeof(T) != 256;          // heads of 128 in bf16 have no registers for them meanwhile
         if (early && !careful) load_columns<T, DH>(cols, K, kl, lane);
         const bool whole = k0 + 31 < sq.n_k && q0 + 31 < sq.n_q && (!causal || k0 + 31 <= pos0);
         const bool near = biased && k0 + 31 - pos0 > -reach && k0 - pos0 - 31 < reach;
@@ -1063,7 +1068,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
 template <typename T, int DH> constexpr bool kOwnInLds = sizeof(T) == 2 && DH == 128;
 template <typename T, int DH, int NW>
 __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<T, DH>) ? 1 : 2) heads_dkv_kernel(AttentionArgs a, const float* __restrict__ stats, Grid grid, float* __restrict__ part) {
-  using Sh = Shape<T, DH>;
+  using Sh = KeyShape<T, DH>;
   constexpr int KB = 32 * NW, QB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const zgr_attention& how = a.how;
@@ -1286,10 +1291,10 @@ __global__ void __launch_bounds__(1024) heads_dbias_kernel(zgr_attention how, co
 }
 
 constexpr int kForwardWaves = 4, kQueryWaves = 4, kKeyWaves = 4;
-template <typename T, int DH> int ring_bytes() { return Shape<T, DH>::ring * 2 * Shape<T, DH>::bytes; }
-template <typename T, int DH> int forward_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + bias_bytes(how); }
-template <typename T, int DH, int NW> int dq_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + bias_bytes(how) + bias_places(how) * 4 * NW; }
-template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return ring_bytes<T, DH>() + Shape<T, DH>::ring * 128 * 4 + (kOwnInLds<T, DH> ? kKeyWaves * 32 * DH * (int)sizeof(T) : 0) + bias_bytes(how); }
+template <typename Sh> int ring_bytes() { return Sh::ring * 2 * Sh::bytes; }
+template <typename T, int DH> int forward_lds(const zgr_attention& how) { return ring_bytes<Shape<T, DH>>() + bias_bytes(how); }
+template <typename T, int DH, int NW> int dq_lds(const zgr_attention& how) { return ring_bytes<Shape<T, DH>>() + bias_bytes(how) + bias_places(how) * 4 * NW; }
+template <typename T, int DH> int dkv_lds(const zgr_attention& how) { return ring_bytes<KeyShape<T, DH>>() + KeyShape<T, DH>::ring * 128 * 4 + (kOwnInLds<T, DH> ? kKeyWaves * 32 * DH * (int)sizeof(T) : 0) + bias_bytes(how); }
 
 template <typename... P, typename... A> hipError_t start(void (*kernel)(P...), int64_t blocks, int threads, int lds, hipStream_t s, A... args) {
   if (!blocks) return hipSuccess;                           // nothing of its kind
