@@ -12,6 +12,7 @@
 #include "sublayer.h"
 #include "wave.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include <type_traits>
@@ -365,7 +366,7 @@ __host__ __device__ inline int bias_bytes(const zgr_attention& h) { return (bias
 // What a block works on: `rank` counts the blocks of a head from the one with the most work (under the causal mask) to the one with the least, `part` the heads that share a unit's K and
 // V (or the slices of its work).  Consecutive block ids go round-robin to the 8 XCDs, each with an L2 of its own.  by_unit: each unit belongs to an XCD, and the blocks with the most work of
 // all its units go first, so that the short ones fill the gaps at the end (paired: the first half, and the second half from its least on); where that would leave XCDs with more units than others, every XCD gets an equal run of blocks, unit by unit.
-struct Grid { int units, parts, ranks, by_unit, paired; };
+struct Grid { int units, parts, ranks, by_unit, paired, slices; };      // slices: of each part of the queries' blocks; the keys' blocks count theirs as parts
 __host__ __device__ inline int64_t blocks_of(const Grid& g) {
   return g.by_unit ? (int64_t)8 * ((g.units + 7) / 8) * g.parts * g.ranks : ((int64_t)g.units * g.parts * g.ranks + 7) / 8 * 8;
 }
@@ -880,7 +881,7 @@ __global__ void __launch_bounds__(256) heads_join_kernel(AttentionArgs a, FewWor
 // ------------------------------------------------------------------------------------------------ backward: dq, the rows' statistics, and the bias gradient's sums by relative position
 // stats: [batch][head][2][stat_rows]: log2 of each row's sum of exponentials, +infinity for a row that has no probabilities, and do . o.
 template <typename T, int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_dq_kernel(AttentionArgs a, float* __restrict__ stats, float* __restrict__ parts, Grid grid) {
+__global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_dq_kernel(AttentionArgs a, float* __restrict__ stats, float* __restrict__ parts, Grid grid, float* __restrict__ sums) {
   using Sh = Shape<T, DH>;
   constexpr int QB = 32 * NW, KB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -888,7 +889,8 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
   [[maybe_unused]] const int qblocks = grid.ranks;
   Place place;
   if (!place_of_block(grid, place)) return;
-  const int qb = qblocks - 1 - place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head, h = hk * grid.parts + place.part;
+  const int qb = qblocks - 1 - place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head, slices = grid.slices, slice = slices > 1 ? place.part % slices : 0;
+  const int h = slices > 1 ? hk * (grid.parts / slices) + place.part / slices : hk * grid.parts + place.part;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
   float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
@@ -900,7 +902,12 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
   const int block_q0 = qb * QB, q0 = block_q0 + group_of<NW>(wave, causal) * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
   int kend = block_q0 < sq.n_q ? sq.n_k : 0;
   if (causal) kend = min(kend, sq.start + min(block_q0 + QB, sq.n_q));
-  const int stages = kend > 0 ? (kend + KB - 1) / KB : 0;
+  const int all_stages = kend > 0 ? (kend + KB - 1) / KB : 0;
+  int first_stage = 0, stages = all_stages;
+  if (slices > 1) {
+    const int per = all_stages / slices, more = all_stages - per * slices;
+    first_stage = slice * per + min(slice, more), stages = per + (slice < more);
+  }
   int wave_kend = q0 < sq.n_q ? kend : 0;
   if (causal) wave_kend = min(wave_kend, pos0 + 32);
   const bool valid = qi < sq.n_q;
@@ -908,7 +915,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
   const T* vbase = row_at<T>(a.v, b, 0, hk);
   auto stage = [&](int st) {
     unsigned char* at = lds + st % Sh::ring * (2 * Sh::bytes);
-    stage_rows<T, DH, KB, NW>(at, kbase, a.k.token, vbase, a.v.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
+    stage_rows<T, DH, KB, NW>(at, kbase, a.k.token, vbase, a.v.token, (first_stage + st) * KB, sq.n_k - 1, how.head_dim, wave, lane);
   };
   const float scale = how.scale * kLog2e;
   Own<T, DH> q, d;
@@ -941,7 +948,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
       const unsigned char* K = lds + st % Sh::ring * (2 * Sh::bytes);
       const unsigned char* V = K + Sh::bytes;
       for (int kl = 0; kl < KB; kl += 32) {
-        const int k0 = st * KB + kl;
+        const int k0 = (first_stage + st) * KB + kl;
         if (k0 >= wave_kend) break;
         if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, valid);
         constexpr bool early = DH * sizeof(T) != 256;          // heads of 128 in bf16 have no registers for the columns meanwhile, nor for a whole row's pieces
@@ -1021,7 +1028,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
     return any_of_block<NW>(bad && valid, lds, wave);
   };
   if (pass(std::false_type())) pass(std::true_type());
-  if (half == 0) {
+  if (half == 0 && (all_stages ? first_stage == 0 && stages : slice == 0)) {      // the slice that has the first tile knows do . o of rows that see no other
     float* stat = stats + ((int64_t)b * how.n_head + h) * 2 * stat_rows(how.n_q) + qi;
     stat[0] = lse;
     stat[stat_rows(how.n_q)] = dot;
@@ -1038,7 +1045,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
       all_bins[j] = v;
     }
     __syncthreads();
-    float* part = parts + (((int64_t)h * how.batch + b) * qblocks + qb) * (2 * reach + 1);
+    float* part = parts + ((((int64_t)h * how.batch + b) * qblocks + qb) * slices + slice) * (2 * reach + 1);
     for (int i = 1 + tid; i < 2 * reach; i += 64 * NW) part[i] = all_bins[i + kBiasPad];
     if (wave < 2) {                                         // wave 0: what lies at -reach and below, wave 1: at reach and above
       const int last = places - 1 - lane;
@@ -1059,6 +1066,10 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
   if (!valid)
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) dq[f] = zeros16();
+  if (slices > 1) {                                         // [slices][batch][n_head][n_q][head_dim], for heads_slices_kernel
+    store_columns<float, DH>(sums + ((((int64_t)slice * how.batch + b) * how.n_head + h) * how.n_q + qi) * how.head_dim, dq, how.scale, half, how.head_dim);
+    return;
+  }
   store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dq, b, qi, h)), dq, how.scale, half, how.head_dim);
 }
 
@@ -1252,21 +1263,20 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<
     for (int f0 = 0; 32 * f0 < how.head_dim; ++f0) pass(std::true_type(), f0);
 }
 
-// dk and dv from their slices' sums, in the slices' order: four entries a thread.
+// dq, or dk and dv, from their slices' sums [of the two][slices][batch][heads][n][dim], in the slices' order: four entries a thread.
 template <typename T>
-__global__ void __launch_bounds__(256) heads_slices_kernel(AttentionArgs a, const float* __restrict__ part, int slices) {
-  const zgr_attention& how = a.how;
-  const int quads = how.head_dim / 4;
-  const int64_t rows = (int64_t)how.batch * how.n_kv_head * how.n_k, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(256) heads_slices_kernel(zgr_heads x0, zgr_heads x1, int heads, int n, int dim, int64_t rows, const float* __restrict__ part, int slices) {
+  const int quads = dim / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= rows * quads) return;
-  const int64_t row = at / quads, unit = row / how.n_k;
-  const int c = (int)(at - row * quads) * 4, key = (int)(row - unit * how.n_k), b = (int)(unit / how.n_kv_head), hk = (int)(unit - (int64_t)b * how.n_kv_head);
-  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(part + (blockIdx.y * (int64_t)slices * rows + row) * how.head_dim + c);
+  const int64_t row = at / quads, unit = row / n;
+  const int c = (int)(at - row * quads) * 4, t = (int)(row - unit * n), b = (int)(unit / heads), h = (int)(unit - (int64_t)b * heads);
+  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(part + (blockIdx.y * (int64_t)slices * rows + row) * dim + c);
   f32x4_t v = *p;
 #pragma unroll 4
   for (int s = 1; s < slices; ++s) v += p[s * rows * quads];
   const float x[4] = {v[0], v[1], v[2], v[3]};
-  store_run(const_cast<T*>(row_at<T>(blockIdx.y ? a.dv : a.dk, b, key, hk)) + c, x);
+  store_run(const_cast<T*>(row_at<T>(blockIdx.y ? x1 : x0, b, t, h)) + c, x);
 }
 
 // ------------------------------------------------------------------------------------------------ dbias: the parts' sums by relative position, then by bucket
@@ -1309,7 +1319,7 @@ Grid grid_of(const zgr_attention& how, int n, int block, int parts) {
   Grid g;
   g.units = how.batch * how.n_kv_head, g.parts = parts, g.ranks = (n + block - 1) / block;
   g.by_unit = (g.units + 7) / 8 * 8 <= g.units + g.units / 8;
-  g.paired = 0;
+  g.paired = 0, g.slices = 1;
   return g;
 }
 // Queries: where all blocks are on the chip at once, two to a compute unit, the shortest stand beside the longest (fp32, 2 x 2048 causal tokens, 16 heads of 64: 217 us forward, so 174; bf16 the same
@@ -1321,6 +1331,17 @@ Grid query_grid(const zgr_attention& how, int waves) {
   return g;
 }
 int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
+// And of dq, where few queries would have few blocks walk many keys: those are cut into slices of four stages at least, up to what the chip holds at once; a slice costs a write and a read of dq in fp32.
+// Backward: 14 queries, 2282 keys, 8 heads of 128, 126 us without, 47 with; 256 on 4096, 2 x 8 heads of 64, 138 and 62; 1500 tokens, 8 heads of 64, 104 and 78; 2048 tokens, 8 heads of 128,
+// both ways 158 and 133, 4 heads of 64 in fp32 334 and 189.
+Grid dq_grid(const zgr_attention& how) {
+  Grid g = query_grid(how, kQueryWaves);
+  const int64_t blocks = (int64_t)g.units * g.ranks * g.parts, held = how.dtype == ZGR_F32 && how.head_dim > 64 ? 256 : 512;
+  int64_t slices = blocks ? (held + blocks / 2) / blocks : 1;
+  slices = std::min(slices, (int64_t)how.n_k / 256);
+  if (slices > 1) g.slices = (int)slices, g.parts *= g.slices, g.paired = 0;
+  return g;
+}
 // Keys: a block walks the queries of every head of its unit.  Where that makes few blocks, whose longest would be waited for, they are cut into slices of equal length, up to as
 // many as the chip holds at once, or twice that under the causal mask, where their lengths differ: slices cost a write and a read of dk and dv in fp32 each.
 // Backward: 2 x 2047 tokens, 32 heads of 128 on 8 (256 blocks), 633 us without, 426 in two, 372 in four; 4096 tokens, 16 heads of 64 on 4 (128 blocks), 667, 278 (four) and 277 (eight); both
@@ -1385,26 +1406,30 @@ template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStre
 }
 
 size_t stats_bytes(const zgr_attention& how) { return ((size_t)how.batch * how.n_head * 2 * (size_t)stat_rows(how.n_q) * 4 + 255) / 256 * 256; }
-int parts_of(const zgr_attention& how) { return how.batch * ((how.n_q + 32 * kQueryWaves - 1) / (32 * kQueryWaves)); }
+int parts_of(const zgr_attention& how) { const Grid g = dq_grid(how); return how.batch * g.ranks * g.slices; }
 
 size_t parts_bytes(const zgr_attention& how) { return how.bias ? ((size_t)parts_of(how) * how.n_head * (2 * (size_t)how.bias_reach + 1) * 4 + 255) / 256 * 256 : 0; }
+// the slices' sums of dq and, behind its kernels in the same place, of dk and dv
 size_t slices_bytes(const zgr_attention& how) {
-  const Grid g = key_grid(how);
-  return g.parts > 1 ? (size_t)2 * g.parts * g.units * how.n_k * how.head_dim * 4 : 0;
+  const Grid q = dq_grid(how), k = key_grid(how);
+  const size_t dq = q.slices > 1 ? (size_t)q.slices * how.batch * how.n_head * how.n_q * how.head_dim * 4 : 0, dkv = k.parts > 1 ? (size_t)2 * k.parts * k.units * how.n_k * how.head_dim * 4 : 0;
+  return std::max(dq, dkv);
+}
+template <typename T> hipError_t join_slices(const zgr_heads& x0, const zgr_heads* x1, const zgr_attention& how, int heads, int n, const float* sums, int slices, hipStream_t s) {
+  const int64_t rows = (int64_t)how.batch * heads * n, quads = rows * (how.head_dim / 4);
+  hipLaunchKernelGGL((heads_slices_kernel<T>), dim3((unsigned)((quads + 255) / 256), x1 ? 2 : 1), dim3(256), 0, s, x0, x1 ? *x1 : x0, heads, n, how.head_dim, rows, sums, slices);
+  return hipGetLastError();
 }
 
 template <typename T, int DH> hipError_t backward(const AttentionArgs& a, hipStream_t s) {
   float* stats = reinterpret_cast<float*>(a.workspace);
   float* parts = a.dbias ? reinterpret_cast<float*>(a.workspace + stats_bytes(a.how)) : nullptr;
-  float* slices = reinterpret_cast<float*>(a.workspace + stats_bytes(a.how) + parts_bytes(a.how));
-  const Grid gq = query_grid(a.how, kQueryWaves), gk = key_grid(a.how);
-  hipError_t e = start(heads_dq_kernel<T, DH, kQueryWaves>, blocks_of(gq), 64 * kQueryWaves, dq_lds<T, DH, kQueryWaves>(a.how), s, a, stats, parts, gq);
-  if (e == hipSuccess) e = start(heads_dkv_kernel<T, DH, kKeyWaves>, blocks_of(gk), 64 * kKeyWaves, dkv_lds<T, DH>(a.how), s, a, (const float*)stats, gk, slices);
-  if (e == hipSuccess && gk.parts > 1) {
-    const int64_t quads = (int64_t)gk.units * a.how.n_k * (a.how.head_dim / 4);
-    hipLaunchKernelGGL((heads_slices_kernel<T>), dim3((unsigned)((quads + 255) / 256), 2), dim3(256), 0, s, a, slices, gk.parts);
-    e = hipGetLastError();
-  }
+  float* sums = reinterpret_cast<float*>(a.workspace + stats_bytes(a.how) + parts_bytes(a.how));
+  const Grid gq = dq_grid(a.how), gk = key_grid(a.how);
+  hipError_t e = start(heads_dq_kernel<T, DH, kQueryWaves>, blocks_of(gq), 64 * kQueryWaves, dq_lds<T, DH, kQueryWaves>(a.how), s, a, stats, parts, gq, sums);
+  if (e == hipSuccess && gq.slices > 1) e = join_slices<T>(a.dq, nullptr, a.how, a.how.n_head, a.how.n_q, sums, gq.slices, s);
+  if (e == hipSuccess) e = start(heads_dkv_kernel<T, DH, kKeyWaves>, blocks_of(gk), 64 * kKeyWaves, dkv_lds<T, DH>(a.how), s, a, (const float*)stats, gk, sums);
+  if (e == hipSuccess && gk.parts > 1) e = join_slices<T>(a.dk, &a.dv, a.how, a.how.n_kv_head, a.how.n_k, sums, gk.parts, s);
   if (e != hipSuccess || !parts) return e;
   hipLaunchKernelGGL((heads_dbias_kernel<T>), dim3(a.how.n_head), dim3(1024), (2 * a.how.bias_reach + 1) * 4, s, a.how, parts, parts_of(a.how), (T*)a.dbias);
   return hipGetLastError();

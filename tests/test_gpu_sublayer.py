@@ -493,6 +493,16 @@ def test_many_queries_over_few_keys(S, dtype, dim, n_k):
     _compare(S, q, k, v, dout, how)
 
 
+@TYPES
+@pytest.mark.parametrize("dim,n_q,n_k", [(64, 14, 1300), (128, 40, 1030), (24, 3, 2100), (64, 300, 700)])
+def test_gradients_of_few_queries_over_many_keys(S, dtype, dim, n_q, n_k):
+    """dq of few blocks, which is summed from slices of its keys; rows that see one tile, or nothing, among them."""
+    q, k, v, dout, how = _inputs(dtype, 2, n_q, n_k, 4, 2, dim, 16, 100, False, seed=n_k)
+    _compare(S, q, k, v, dout, how)
+    how.update(causal=True, q_start=torch.tensor([n_k - n_q, -1], dtype=torch.int32, device="cuda"), k_lengths=torch.tensor([n_k - 5, n_k // 2], dtype=torch.int32, device="cuda"))
+    _compare(S, q, k, v, dout, how)
+
+
 def test_in_a_graph(S):
     """Every operator captured once and replayed on new inputs, with the caller's own work between the replays."""
     g = _gen(3)
