@@ -464,7 +464,7 @@ template <int DH> __device__ __forceinline__ void raise_maximum(float top, float
 
 // ------------------------------------------------------------------------------------------------ forward
 template <typename T, int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs a, Grid grid) {
+__global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs a, Grid grid, float* __restrict__ sums) {
   using Sh = Shape<T, DH>;
   constexpr int QB = 32 * NW, KB = Sh::rows, PER = 2 * Sh::bytes / (1024 * NW);      // PER: transfers of a wave for a stage
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -472,7 +472,8 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
   [[maybe_unused]] const int qblocks = grid.ranks;
   Place place;
   if (!place_of_block(grid, place)) return;
-  const int qb = qblocks - 1 - place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head, h = hk * grid.parts + place.part;
+  const int qb = qblocks - 1 - place.rank, b = place.unit / how.n_kv_head, hk = place.unit - b * how.n_kv_head, slices = grid.slices, slice = slices > 1 ? place.part % slices : 0;
+  const int h = slices > 1 ? hk * (grid.parts / slices) + place.part / slices : hk * grid.parts + place.part;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_of(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const Sequence sq = sequence_of(how, b);
   float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
@@ -481,14 +482,19 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
   const int block_q0 = qb * QB, q0 = block_q0 + group_of<NW>(wave, causal) * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
   int kend = block_q0 < sq.n_q ? sq.n_k : 0;
   if (causal) kend = min(kend, sq.start + min(block_q0 + QB, sq.n_q));
-  const int stages = kend > 0 ? (kend + KB - 1) / KB : 0;
+  const int all_stages = kend > 0 ? (kend + KB - 1) / KB : 0;
+  int first_stage = 0, stages = all_stages;
+  if (slices > 1) {
+    const int per = all_stages / slices, more = all_stages - per * slices;
+    first_stage = slice * per + min(slice, more), stages = per + (slice < more);
+  }
   int wave_kend = q0 < sq.n_q ? kend : 0;
   if (causal) wave_kend = min(wave_kend, pos0 + 32);
   const T* kbase = row_at<T>(a.k, b, 0, hk);
   const T* vbase = row_at<T>(a.v, b, 0, hk);
   auto stage = [&](int st) {                                // stages past the last are transferred as well (its last row again): every wave then counts the same transfers
     unsigned char* at = lds + st % Sh::ring * (2 * Sh::bytes);
-    stage_rows<T, DH, KB, NW>(at, kbase, a.k.token, vbase, a.v.token, st * KB, sq.n_k - 1, how.head_dim, wave, lane);
+    stage_rows<T, DH, KB, NW>(at, kbase, a.k.token, vbase, a.v.token, (first_stage + st) * KB, sq.n_k - 1, how.head_dim, wave, lane);
   };
   const float scale = how.scale * kLog2e;
   Own<T, DH> q;
@@ -513,7 +519,7 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
       const unsigned char* K = lds + st % Sh::ring * (2 * Sh::bytes);
       const unsigned char* V = K + Sh::bytes;
       for (int kl = 0; kl < KB; kl += 32) {
-        const int k0 = st * KB + kl;
+        const int k0 = (first_stage + st) * KB + kl;
         if (k0 >= wave_kend) break;
         if (careful) load_own<T, DH>(q, row_at<T>(a.q, b, qi, h), half, how.head_dim, qi < sq.n_q);      // so that it takes no registers beside columns_exactly's
         const f32x16 s = rows_product<T, DH>(K, kl, q, l32, half);
@@ -578,12 +584,46 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
   if (qi >= how.n_q) return;
   lsum = both_halves(lsum);
   const bool none = qi >= sq.n_q || lsum == 0.f;
+  if (slices > 1) {                                         // [slices][batch][n_head][n_q][head_dim], and behind them [slices][batch][n_head][n_q][2], for heads_parts_kernel
+    const int64_t rows = (int64_t)how.batch * how.n_head * how.n_q, at = slice * rows + ((int64_t)b * how.n_head + h) * how.n_q + qi;
+    store_columns<float, DH>(sums + at * how.head_dim, o, none ? 0.f : 1.0f, half, how.head_dim);
+    if (half == 0) {
+      float* st = sums + slices * rows * how.head_dim + at * 2;
+      st[0] = none ? -INFINITY : mx;
+      st[1] = none ? 0.f : lsum;
+    }
+    return;
+  }
   T* row = const_cast<T*>(row_at<T>(a.out, b, qi, h));
   if (none)
 #pragma unroll
     for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
   store_columns<T, DH>(row, o, none ? 0.f : 1.0f / lsum, half, how.head_dim);
   if (half == 0) a.lse[((int64_t)b * how.n_head + h) * how.n_q + qi] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(lsum)) * kLn2;
+}
+
+// The rows of the forward pass from their slices, in the slices' order: four entries a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) heads_parts_kernel(AttentionArgs a, const float* __restrict__ sums, int slices) {
+  const zgr_attention& how = a.how;
+  const int quads = how.head_dim / 4;
+  const int64_t rows = (int64_t)how.batch * how.n_head * how.n_q, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= rows * quads) return;
+  const int64_t row = at / quads, unit = row / how.n_q;
+  const int c = (int)(at - row * quads) * 4, t = (int)(row - unit * how.n_q), b = (int)(unit / how.n_head), h = (int)(unit - (int64_t)b * how.n_head);
+  const float* stats = sums + slices * rows * how.head_dim + row * 2;
+  float m = -INFINITY, l = 0.f;
+  for (int s = 0; s < slices; ++s) m = fmaxf(m, stats[s * rows * 2]);
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < slices && m != -INFINITY; ++s) {
+    const float w = __builtin_amdgcn_exp2f(stats[s * rows * 2] - m);
+    if (w == 0.f) continue;                                 // a slice without a visible key left nothing to weigh
+    l = __builtin_fmaf(w, stats[s * rows * 2 + 1], l);
+    v += w * *reinterpret_cast<const f32x4_t*>(sums + (s * rows + row) * how.head_dim + c);
+  }
+  const float by = m == -INFINITY ? 0.f : 1.0f / l, x[4] = {v[0] * by, v[1] * by, v[2] * by, v[3] * by};
+  store_run(const_cast<T*>(row_at<T>(a.out, b, t, h)) + c, x);
+  if (c == 0) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------------------------ forward, few queries over many keys
@@ -1331,17 +1371,26 @@ Grid query_grid(const zgr_attention& how, int waves) {
   return g;
 }
 int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
-// And of dq, where few queries would have few blocks walk many keys: those are cut into slices of four stages at least, up to what the chip holds at once; a slice costs a write and a read of dq in fp32.
+// Where few queries would have few blocks walk many keys, those are cut into slices of four stages at least, up to what the chip holds at once; a slice costs a write and a read of the result in fp32.
 // Backward: 14 queries, 2282 keys, 8 heads of 128, 126 us without, 47 with; 256 on 4096, 2 x 8 heads of 64, 138 and 62; 1500 tokens, 8 heads of 64, 104 and 78; 2048 tokens, 8 heads of 128,
-// both ways 158 and 133, 4 heads of 64 in fp32 334 and 189.
-Grid dq_grid(const zgr_attention& how) {
-  Grid g = query_grid(how, kQueryWaves);
-  const int64_t blocks = (int64_t)g.units * g.ranks * g.parts, held = how.dtype == ZGR_F32 && how.head_dim > 64 ? 256 : 512;
+// both ways 158 and 133, 4 heads of 64 in fp32 334 and 189.  Forward, where a share of 12 us at least is saved: 256 on 4096 62 and 35; 300 on 8192, 8 heads of 128, 74 and 49; 1500 tokens 36
+// and 29; 2048 tokens, 8 heads of 128, 66 and 46, 4 of 64 in fp32 101 and 59; 1040 tokens, 24 heads of 32, which it leaves whole, 23 and 27.
+Grid sliced_grid(const zgr_attention& how, int waves, int64_t held) {
+  Grid g = query_grid(how, waves);
+  const int64_t blocks = (int64_t)g.units * g.ranks * g.parts;
   int64_t slices = blocks ? (held + blocks / 2) / blocks : 1;
   slices = std::min(slices, (int64_t)how.n_k / 256);
   if (slices > 1) g.slices = (int)slices, g.parts *= g.slices, g.paired = 0;
   return g;
 }
+constexpr double kSlicesUs = 12;                            // what the slices' sums, and the launch that joins them, cost the forward pass at least
+double tile_us(const zgr_attention& how) { return how.dtype == ZGR_F32 ? (how.head_dim > 64 ? 4.5 : 2.4) : (how.head_dim > 64 ? 1.0 : 0.57); }      // a block's, of 32 keys, measured
+Grid forward_grid(const zgr_attention& how) {
+  const Grid one = query_grid(how, kForwardWaves), g = sliced_grid(how, kForwardWaves, 512);
+  const double tiles = (how.n_k + 31) / 32;
+  return tiles * tile_us(how) * (1 - 1.0 / g.slices) > kSlicesUs ? g : one;
+}
+Grid dq_grid(const zgr_attention& how) { return sliced_grid(how, kQueryWaves, how.dtype == ZGR_F32 && how.head_dim > 64 ? 256 : 512); }
 // Keys: a block walks the queries of every head of its unit.  Where that makes few blocks, whose longest would be waited for, they are cut into slices of equal length, up to as
 // many as the chip holds at once, or twice that under the causal mask, where their lengths differ: slices cost a write and a read of dk and dv in fp32 each.
 // Backward: 2 x 2047 tokens, 32 heads of 128 on 8 (256 blocks), 633 us without, 426 in two, 372 in four; 4096 tokens, 16 heads of 64 on 4 (128 blocks), 667, 278 (four) and 277 (eight); both
@@ -1356,17 +1405,18 @@ Grid key_grid(const zgr_attention& how) {
   return g;
 }
 
-// Which of the two forward kernels: the sooner done by an estimate.  Blocks of queries walk all keys, 0.57 us (bf16, heads up to 64), 1.0 (128), 2.4 and 4.5 (fp32) a tile of 32, some
-// 768 blocks at a time.  Runs of tiles take 4 us for each 8 KiB tile of a worker's run, of which there are 2048 (1024), and 8 us more to begin with (the count, and the launch that joins
+// Which of the two forward kernels: the sooner done by an estimate.  Blocks of queries walk all keys, or a slice of them, 0.57 us (bf16, heads up to 64), 1.0 (128), 2.4 and 4.5
+// (fp32) a tile of 32, some 768 blocks at a time.  Runs of tiles take 4 us for each 8 KiB tile of a worker's run, of which there are 2048 (1024), and 8 us more to begin with (the count, and the launch that joins
 // them).  Measured, blocks | runs: 1 query, 8 heads of 64, 1024 keys 23.7 | 14.1 us, 128 keys 7.7 | 13.8; 16 x 1 query, 32 heads of 128 on 8, 1024 keys 37.5 | 28.9, 256 keys 14.8 | 19.8;
 // 512 queries, 4 heads of 64, 4096 keys 85.6 | 39.0; 1500 queries on themselves, 8 heads 35.6 | 70.1; fp32, 16 x 16 queries, 8 heads of 64, 256 keys 25.4 | 22.8.
 bool few_queries(const zgr_attention& how) {
   if (!how.n_k || !how.n_q || !how.batch) return false;
   const int dim = padded_dim(how.head_dim), bytes = dim * (how.dtype == ZGR_F32 ? 4 : 2);
   const double tiles = (how.n_k + 31) / 32, rows = (double)(how.n_head / how.n_kv_head) * how.n_q;
-  const double blocks = (double)((how.n_q + 32 * kForwardWaves - 1) / (32 * kForwardWaves)) * how.n_head * how.batch, tile_us = how.dtype == ZGR_F32 ? (dim > 64 ? 4.5 : 2.4) : (dim > 64 ? 1.0 : 0.57);
+  const Grid g = forward_grid(how);
+  const double blocks = (double)g.units * g.ranks * g.parts, walk = std::ceil(tiles / g.slices) * tile_us(how) * std::fmax(1.0, blocks / 768) + (g.slices > 1 ? kSlicesUs : 0);
   const double items = std::ceil(rows / 32) * how.n_kv_head * how.batch, workers = bytes > 256 ? 1024 : 2048;
-  return 8 + std::ceil(items * tiles / workers) * 4 * (bytes / 128.0) < tiles * tile_us * std::fmax(1.0, blocks / 768);
+  return 8 + std::ceil(items * tiles / workers) * 4 * (bytes / 128.0) < walk;
 }
 int few_resident(const zgr_attention& how) { return how.dtype == ZGR_F32 && how.head_dim > 64 ? FewShape<float, 128>::resident : FewShape<float, 64>::resident; }
 FewWork few_work(const zgr_attention& how, bool& even) {
@@ -1384,8 +1434,11 @@ template <typename T, int DH> size_t part_bytes(const zgr_attention& how) {
   const FewWork w = few_work(how, even);
   return even ? (size_t)w.workers * 2 * w.rows * (DH + 2) * 4 : 0;
 }
-size_t few_bytes(const zgr_attention& how) {
-  if (!few_queries(how)) return 0;
+size_t forward_bytes(const zgr_attention& how) {
+  if (!few_queries(how)) {
+    const Grid g = forward_grid(how);
+    return g.slices > 1 ? (size_t)g.slices * how.batch * how.n_head * how.n_q * (how.head_dim + 2) * 4 : 0;
+  }
   const int d = padded_dim(how.head_dim);
   const size_t part = d == 32 ? part_bytes<float, 32>(how) : d == 64 ? part_bytes<float, 64>(how) : part_bytes<float, 128>(how);
   return part ? (part + 255) / 256 * 256 + ((size_t)how.batch + 1) * 4 : 0;
@@ -1393,8 +1446,11 @@ size_t few_bytes(const zgr_attention& how) {
 
 template <typename T, int DH> hipError_t forward(const AttentionArgs& a, hipStream_t s) {
   if (!few_queries(a.how)) {
-    const Grid g = query_grid(a.how, kForwardWaves);
-    return start(heads_forward_kernel<T, DH, kForwardWaves>, blocks_of(g), 64 * kForwardWaves, forward_lds<T, DH>(a.how), s, a, g);
+    const Grid g = forward_grid(a.how);
+    float* sums = reinterpret_cast<float*>(a.workspace);
+    const hipError_t e = start(heads_forward_kernel<T, DH, kForwardWaves>, blocks_of(g), 64 * kForwardWaves, forward_lds<T, DH>(a.how), s, a, g, sums);
+    if (e != hipSuccess || g.slices < 2) return e;
+    return start(heads_parts_kernel<T>, ((int64_t)a.how.batch * a.how.n_head * a.how.n_q * (a.how.head_dim / 4) + 255) / 256, 256, 0, s, a, (const float*)sums, g.slices);
   }
   bool even;
   const FewWork w = few_work(a.how, even);
@@ -1437,7 +1493,7 @@ template <typename T, int DH> hipError_t backward(const AttentionArgs& a, hipStr
 
 }  // namespace
 
-size_t attention_workspace(const zgr_attention& how) { return few_bytes(how); }
+size_t attention_workspace(const zgr_attention& how) { return forward_bytes(how); }
 size_t attention_backward_workspace(const zgr_attention& how) { return stats_bytes(how) + parts_bytes(how) + slices_bytes(how); }
 
 hipError_t launch_heads_forward(const AttentionArgs& a, hipStream_t s) {

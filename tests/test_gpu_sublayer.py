@@ -503,6 +503,20 @@ def test_gradients_of_few_queries_over_many_keys(S, dtype, dim, n_q, n_k):
     _compare(S, q, k, v, dout, how)
 
 
+@TYPES
+@pytest.mark.parametrize("dim,n_q,n_k,heads,kv_heads", [(128, 200, 2100, 2, 1), (64, 400, 1700, 2, 2), (24, 260, 2600, 4, 2)])
+def test_few_blocks_over_many_keys(S, dtype, dim, n_q, n_k, heads, kv_heads):
+    """Rows that are summed from slices of their keys; some see one tile, some nothing, some hidden NaN."""
+    q, k, v, dout, how = _inputs(dtype, 2, n_q, n_k, heads, kv_heads, dim, 16, 100, False, seed=n_k)
+    _compare(S, q, k, v, dout, how, grads=False)
+    how.update(causal=True, q_start=torch.tensor([n_k - n_q, -3], dtype=torch.int32, device="cuda"), k_lengths=torch.tensor([n_k - 5, n_k // 2], dtype=torch.int32, device="cuda"))
+    out, lse = R.attention(q, k, v, **how)
+    k[0, n_k - 5:], v[0, n_k - 5:], v[1, n_q - 3:] = math.nan, math.inf, math.nan
+    got = S.attention(q, k, v, **how)
+    R.check(got[0], out, "out")
+    R.check(got[1], lse, "lse")
+
+
 def test_in_a_graph(S):
     """Every operator captured once and replayed on new inputs, with the caller's own work between the replays."""
     g = _gen(3)
