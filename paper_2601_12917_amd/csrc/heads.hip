@@ -1371,15 +1371,17 @@ Grid query_grid(const zgr_attention& how, int waves) {
   return g;
 }
 int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
-// Where few queries would have few blocks walk many keys, those are cut into slices of four stages at least, up to what the chip holds at once; a slice costs a write and a read of the result in fp32.
+// Where few queries would have few blocks walk many keys, those are cut into slices, up to what the chip holds at once; a slice costs a write and a read of the result in fp32.
 // Backward: 14 queries, 2282 keys, 8 heads of 128, 126 us without, 47 with; 256 on 4096, 2 x 8 heads of 64, 138 and 62; 1500 tokens, 8 heads of 64, 104 and 78; 2048 tokens, 8 heads of 128,
 // both ways 158 and 133, 4 heads of 64 in fp32 334 and 189.  Forward, where a share of 12 us at least is saved: 256 on 4096 62 and 35; 300 on 8192, 8 heads of 128, 74 and 49; 1500 tokens 36
 // and 29; 2048 tokens, 8 heads of 128, 66 and 46, 4 of 64 in fp32 101 and 59; 1040 tokens, 24 heads of 32, which it leaves whole, 23 and 27.
+// Rows that a slice walks at least: some 5 to 10 us of a block (256 for fp32 too: backward of 3 x 406 tokens, one head of 128, 239 us for 90, 2 x 300, 4 of 64, 114 for 76).
+int least_walk(const zgr_attention& how) { return how.dtype == ZGR_BF16 ? 256 : how.head_dim <= 64 ? 128 : 64; }
 Grid sliced_grid(const zgr_attention& how, int waves, int64_t held) {
   Grid g = query_grid(how, waves);
   const int64_t blocks = (int64_t)g.units * g.ranks * g.parts;
   int64_t slices = blocks ? (held + blocks / 2) / blocks : 1;
-  slices = std::min(slices, (int64_t)how.n_k / 256);
+  slices = std::min(slices, (int64_t)how.n_k / least_walk(how));
   if (slices > 1) g.slices = (int)slices, g.parts *= g.slices, g.paired = 0;
   return g;
 }
@@ -1397,10 +1399,10 @@ Grid dq_grid(const zgr_attention& how) { return sliced_grid(how, kQueryWaves, ho
 // ways 1500 tokens, 8 heads of 64 (96 blocks), 139 and 104 (five); 8 x 512 tokens, 16 heads of 128 (512 blocks), 114, and in two 156.
 Grid key_grid(const zgr_attention& how) {
   Grid g = grid_of(how, how.n_k, 32 * kKeyWaves, 1);
-  const int64_t blocks = (int64_t)g.units * g.ranks, walk = (int64_t)((how.n_q + 63) / 64) * (how.n_head / how.n_kv_head);
+  const int64_t blocks = (int64_t)g.units * g.ranks, walk = (int64_t)how.n_q * (how.n_head / how.n_kv_head);
   const int64_t held = how.dtype == ZGR_F32 && how.head_dim > 32 ? 256 : 512, wanted = how.causal ? 2 * held : held;
   int64_t slices = blocks ? (wanted + blocks / 2) / blocks : 1;
-  if (slices > walk / 4) slices = walk / 4;
+  slices = std::min(slices, walk / least_walk(how));
   g.parts = slices < 1 ? 1 : (int)slices;
   return g;
 }
