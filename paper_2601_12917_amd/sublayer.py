@@ -13,7 +13,8 @@ from . import binding as B
 
 _DTYPES = {torch.float32: B.ZGR_F32, torch.bfloat16: B.ZGR_BF16}
 _U64 = (1 << 64) - 1
-_heads, _ref = B.zgr_heads, C.byref
+_heads = B.zgr_heads
+_empty_like, _CONTIGUOUS = torch.empty_like, torch.contiguous_format      # half of what torch.empty with a shape, type and device takes
 try:
     _stream_of = torch._C._cuda_getCurrentRawStream      # torch.cuda.current_stream(i).cuda_stream without the object around it: 0.1 us, not 2
 except AttributeError:
@@ -59,10 +60,11 @@ def _view(t, name, like=None):
 
 def _new(t):
     """Memory for a result of t's shape and type, rows one behind the other, and its zgr_heads."""
+    out = _empty_like(t, memory_format=_CONTIGUOUS)
     shape = t.shape
-    out = torch.empty(shape, dtype=t.dtype, device=t.device)
-    row = shape[-1] * shape[-2]
-    return out, _heads(out.data_ptr(), row * shape[-3], row, shape[-1])
+    dim = shape[-1]
+    row = dim * shape[-2]
+    return out, _heads(out.data_ptr(), row * shape[-3], row, dim)
 
 
 def _call(device, call, *args):
@@ -189,7 +191,7 @@ def attention_backward(dout, q, k, v, out, lse, bias=None, bias_map=None, causal
         raise ValueError("lse: what attention returned")
     views = _view(dout, "dout", q), _view(q, "q"), _view(k, "k"), _view(v, "v"), _view(out, "out", q)
     (dq, dqv), (dk, dkv), (dv, dvv) = _new(q), _new(k), _new(v)
-    dbias = None if bias is None else torch.empty(bias.shape, dtype=bias.dtype, device=dev)
+    dbias = None if bias is None else _empty_like(bias, memory_format=_CONTIGUOUS)
     lib = B.lib()
     n = lib.zgr_attention_backward_workspace(how)
     ws = torch.empty(n, dtype=torch.uint8, device=dev)
