@@ -447,10 +447,6 @@ template <int NW> __device__ __forceinline__ bool any_of_block(bool mine, unsign
   return yes;
 }
 
-// Which queries a block works on.  Under the causal mask a block's work grows with its position and a wave's with its queries': blocks go longest first, and with eight waves, of
-// which w and w + 4 share a SIMD, the upper four take their queries in reverse order.
-template <int NW> __device__ __forceinline__ int group_of(int wave, int causal) { return NW == 8 && causal && wave >= 4 ? 11 - wave : wave; }
-
 // The maximum that the exponentials are taken against follows a tile's only where that is more than 2^8 times as large: sums and probabilities of up to 2^8 keep their relative
 // rounding, and past the first tiles nothing is rescaled (with the maximum itself one of 32 rows moves it in 40 % of the tiles after 64 of them).
 template <int DH> __device__ __forceinline__ void raise_maximum(float top, float& mx, float& lsum, f32x16 (&o)[DH / 32]) {
@@ -463,6 +459,9 @@ template <int DH> __device__ __forceinline__ void raise_maximum(float top, float
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[f][v] *= corr;
 }
+
+// The maximum that a part of a row's keys leaves for the join: of a part whose every score is NaN, +infinity, so that its sum is not passed over but makes the row NaN.
+__device__ __forceinline__ float part_maximum(bool none, float mx, float lsum) { return none ? -INFINITY : lsum != lsum ? INFINITY : mx; }
 
 // ------------------------------------------------------------------------------------------------ forward
 // Two products a tile, 32 x 32 x DH each, and some 150 vector instructions between them, 16 of which are exponentials at a quarter of the rate: vector and matrix instructions take
@@ -484,7 +483,7 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
   float* by_delta = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes);
   const bool biased = how.bias != nullptr;
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_q0 = qb * QB, q0 = block_q0 + group_of<NW>(wave, causal) * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
+  const int block_q0 = qb * QB, q0 = block_q0 + wave * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
   int kend = block_q0 < sq.n_q ? sq.n_k : 0;
   if (causal) kend = min(kend, sq.start + min(block_q0 + QB, sq.n_q));
   const int all_stages = kend > 0 ? (kend + KB - 1) / KB : 0;
@@ -594,15 +593,12 @@ __global__ void __launch_bounds__(64 * NW, 2) heads_forward_kernel(AttentionArgs
     store_columns<float, DH>(sums + at * how.head_dim, o, none ? 0.f : 1.0f, half, how.head_dim);
     if (half == 0) {
       float* st = sums + slices * rows * how.head_dim + at * 2;
-      st[0] = none ? -INFINITY : mx;
+      st[0] = part_maximum(none, mx, lsum);
       st[1] = none ? 0.f : lsum;
     }
     return;
   }
   T* row = const_cast<T*>(row_at<T>(a.out, b, qi, h));
-  if (none)
-#pragma unroll
-    for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
   store_columns<T, DH>(row, o, none ? 0.f : 1.0f / lsum, half, how.head_dim);
   if (half == 0) a.lse[((int64_t)b * how.n_head + h) * how.n_q + qi] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(lsum)) * kLn2;
 }
@@ -848,16 +844,13 @@ __global__ void __launch_bounds__(64, DH * sizeof(T) >= 512 ? 1 : 2) heads_few_k
     lsum = both_halves(lsum);
     const bool none = i >= sq.n_q || lsum == 0.f;
     if (r < rows && begins && ends) {
-      if (none)
-#pragma unroll
-        for (int f = 0; f < DH / 32; ++f) o[f] = zeros16();
       store_columns<T, DH>(const_cast<T*>(row_at<T>(a.out, b, i, h)), o, none ? 0.f : 1.0f / lsum, half, how.head_dim);
       if (half == 0) a.lse[((int64_t)b * how.n_head + h) * how.n_q + i] = none ? -INFINITY : (mx + __builtin_amdgcn_logf(lsum)) * kLn2;
     } else if (r < rows) {
       const int64_t row = ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * w.rows + l32;
       if (half == 0) {
         float* st = part + (int64_t)w.workers * 2 * w.rows * DH + row * 2;
-        st[0] = none ? -INFINITY : mx;
+        st[0] = part_maximum(none, mx, lsum);
         st[1] = none ? 0.f : lsum;
       }
       if (!none) store_columns<float, DH>(part + row * DH, o, 1.0f, half, DH);      // not read otherwise
@@ -948,7 +941,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
   float* all_bins = reinterpret_cast<float*>(lds + Sh::ring * 2 * Sh::bytes + bias_bytes(how));
   float* bins = all_bins + wave * places;                   // each wave's sums by relative position
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_q0 = qb * QB, q0 = block_q0 + group_of<NW>(wave, causal) * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
+  const int block_q0 = qb * QB, q0 = block_q0 + wave * 32, qi = q0 + l32, pos = sq.start + qi, pos0 = sq.start + q0;
   int kend = block_q0 < sq.n_q ? sq.n_k : 0;
   if (causal) kend = min(kend, sq.start + min(block_q0 + QB, sq.n_q));
   const int all_stages = kend > 0 ? (kend + KB - 1) / KB : 0;
@@ -1112,14 +1105,11 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) == 512 ? 1 : 2) heads_
     }
   }
   if (qi >= how.n_q) return;
-  if (!valid)
-#pragma unroll
-    for (int f = 0; f < DH / 32; ++f) dq[f] = zeros16();
   if (slices > 1) {                                         // [slices][batch][n_head][n_q][head_dim], for heads_slices_kernel
-    store_columns<float, DH>(sums + ((((int64_t)slice * how.batch + b) * how.n_head + h) * how.n_q + qi) * how.head_dim, dq, how.scale, half, how.head_dim);
+    store_columns<float, DH>(sums + ((((int64_t)slice * how.batch + b) * how.n_head + h) * how.n_q + qi) * how.head_dim, dq, valid ? how.scale : 0.f, half, how.head_dim);
     return;
   }
-  store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dq, b, qi, h)), dq, how.scale, half, how.head_dim);
+  store_columns<T, DH>(const_cast<T*>(row_at<T>(a.dq, b, qi, h)), dq, valid ? how.scale : 0.f, half, how.head_dim);
 }
 
 // ------------------------------------------------------------------------------------------------ backward: dk, dv
@@ -1145,7 +1135,7 @@ __global__ void __launch_bounds__(64 * NW, DH * sizeof(T) >= 256 && !(kOwnInLds<
   float* by_delta = rows_stats + Sh::ring * 128 + (own_in_lds ? NW * 32 * DH * (int)sizeof(T) / 4 : 0);
   const bool biased = how.bias != nullptr;
   const int reach = how.bias_reach, causal = how.causal;
-  const int block_k0 = kb * KB, k0 = block_k0 + group_of<NW>(wave, causal) * 32;
+  const int block_k0 = kb * KB, k0 = block_k0 + wave * 32;
   // the first query that sees a key of the block, and of the wave
   int qbegin = causal ? max(0, block_k0 - sq.start) : 0, wave_qbegin = causal ? max(0, k0 - sq.start) : 0;
   if (block_k0 >= sq.n_k) qbegin = sq.n_q;

@@ -517,6 +517,26 @@ def test_few_blocks_over_many_keys(S, dtype, dim, n_q, n_k, heads, kv_heads):
     R.check(got[1], lse, "lse")
 
 
+@TYPES
+@pytest.mark.parametrize("n_q", [1, 200])
+def test_nan_that_is_seen_comes_through_slices(S, dtype, n_q):
+    """Rows all of whose scores are NaN, in every slice of their keys or in some: not zeros, and no row beside them."""
+    q, k, v, dout, how = _inputs(dtype, 2, n_q, 2100, 2, 1, 64, 16, 100, False, seed=n_q)
+    want = S.attention(q, k, v, **how)
+    bad = q.clone()
+    bad[1, n_q - 1, 1, 5] = math.nan
+    out, lse = S.attention(bad, k, v, **how)
+    assert out[1, n_q - 1, 1].isnan().all() and lse[1, 1, n_q - 1].isnan()
+    fine = torch.ones(2, n_q, 2, dtype=torch.bool, device="cuda")
+    fine[1, n_q - 1, 1] = False
+    assert out[fine].isfinite().all() and lse.transpose(1, 2)[fine].isfinite().all()
+    R.check(out[fine], want[0][fine], "out")
+    keys = k.clone()
+    keys[0, :1000] = math.nan
+    out, lse = S.attention(q, keys, v, **how)
+    assert out[0].isnan().all() and lse[0].isnan().all() and torch.equal(out[1], want[0][1])
+
+
 def test_in_a_graph(S):
     """Every operator captured once and replayed on new inputs, with the caller's own work between the replays."""
     g = _gen(3)
