@@ -1411,7 +1411,7 @@ Grid key_grid(const zgr_attention& how) {
 // Which of the two forward kernels: the sooner done by an estimate.  Blocks of queries walk all keys, or a slice of them, 0.57 us (bf16, heads up to 64), 1.0 (128), 2.4 and 4.5
 // (fp32) a tile of 32, some 768 blocks at a time.  Runs of tiles take 4 us for each 8 KiB tile of a worker's run, of which there are 2048 (1024), and 8 us more to begin with (the count, and the launch that joins
 // them).  Measured, blocks | runs: 1 query, 8 heads of 64, 1024 keys 23.7 | 14.1 us, 128 keys 7.7 | 13.8; 16 x 1 query, 32 heads of 128 on 8, 1024 keys 37.5 | 28.9, 256 keys 14.8 | 19.8;
-// 512 queries, 4 heads of 64, 4096 keys 85.6 | 39.0; 1500 queries on themselves, 8 heads 35.6 | 70.1; fp32, 16 x 16 queries, 8 heads of 64, 256 keys 25.4 | 22.8.
+// 512 queries, 4 heads of 64, 4096 keys 85.6, in slices 29.9 | 39.0; 1500 queries on themselves, 8 heads 35.6 | 70.1; fp32, 16 x 16 queries, 8 heads of 64, 256 keys 25.4 | 22.8.
 bool few_queries(const zgr_attention& how) {
   if (!how.n_k || !how.n_q || !how.batch) return false;
   const int dim = padded_dim(how.head_dim), bytes = dim * (how.dtype == ZGR_F32 ? 4 : 2);

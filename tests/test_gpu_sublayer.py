@@ -567,3 +567,28 @@ def test_in_a_graph(S):
         torch.cuda.synchronize()
         for i, (a, b) in enumerate(zip(held, work())):
             assert torch.equal(a, b), i
+
+
+@TYPES
+@pytest.mark.parametrize("n_q,n_k", [(1, 3000), (150, 1400)], ids=["one token", "slices"])
+def test_large_heads_in_a_graph(S, dtype, n_q, n_k):
+    """Heads of 128, whose blocks ask for more LDS than a launch gives by itself, with joins behind them."""
+    q, k, v, dout, how = _inputs(dtype, 2, n_q, n_k, 4, 2, 128, 16, 100, True, seed=n_q)
+    lengths = torch.tensor([n_k, n_k - 700], dtype=torch.int32, device="cuda")
+    how.update(k_lengths=lengths, q_start=lengths - n_q)
+
+    def work():
+        out, lse = S.attention(q, k, v, **how)
+        return (out, lse, *S.attention_backward(dout, q, k, v, out, lse, **how))
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = work()
+    for seed in range(3):
+        for t, n in zip((q, k, v, dout), _inputs(dtype, 2, n_q, n_k, 4, 2, 128, seed=seed)):
+            t.copy_(n)
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(held, work())):
+            assert torch.equal(a, b), i
